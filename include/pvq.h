@@ -306,6 +306,102 @@ int pvq_decode_gemv(const pvq_ctx *ctx, const uint32_t *index, const void *scale
                     const float *rownorm, int64_t rows, int64_t cols, const void *x, int batch,
                     int64_t ldx, float *y, int64_t ldy, void *stream);
 
+/* ---- 8-bit blocks: products of many rows, and training ----------------------------------------- */
+
+/*
+ * A block matrix [rows][cols] holds its values as 8-bit floating point numbers (e4m3: sign, four exponent bits, three
+ * fraction bits, largest 448, no infinities) with a power of two for every 128 neighbouring values of a row:
+ *   - codes: uint8 [rows][C], C = 128 ceil(cols/128); the codes behind a row's last column are zero.
+ *   - exponents: uint8 [rows][E], E = 4 ceil(C/128/4); byte b of a row stands for the scale 2^(b - 127) of that block of
+ *     128 codes, the bytes behind a row's last block are zero.
+ * value = code * scale.  It is what pvq_decode's weights and the activations become for products with more rows than
+ * pvq_decode_gemv takes, and what a training step keeps of its activations.  Powers of two, because the matrix
+ * instruction multiplies them in by itself, and because every decoded value is then exact in bfloat16.
+ *
+ * Everywhere below: codes 16-byte aligned, exponents 4-byte aligned; matrices of floats aligned to their element, any ld >= cols
+ * (rows that are aligned to 16 bytes are faster); rows or cols may be 0; columns of a block matrix at most 4194304 (2^22),
+ * rows at most 2^30 and values 2^41, else PVQ_E_UNSUPPORTED.
+ * Calls are asynchronous, launch kernels on `stream` only and may be captured.  NaN codes give NaN; codes behind the last
+ * column that are not zero and exponent bytes outside 17 .. 247 (which encoding never writes) give unspecified values, never
+ * an out-of-bounds access.
+ */
+
+/* Bytes of the two planes (host out pointers, may be NULL). */
+int pvq_fp8_sizes(int64_t rows, int64_t cols, size_t *code_bytes, size_t *exponent_bytes);
+
+/*
+ * A matrix to blocks.  A block's scale is 2^s with the least integer s for which its largest finite magnitude is at most
+ * 448 * 2^s, -110 <= s <= 120; a code is value / 2^s rounded to nearest, ties to even.  Infinities and NaN become NaN
+ * codes and do not count for the scale.
+ *   X   device, [rows][ldx] of dtype (PVQ_F32, PVQ_F16 or PVQ_BF16)
+ */
+int pvq_fp8_encode(const void *X, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes, uint8_t *exponents,
+                   void *stream);
+
+/* Blocks to a matrix: exact in PVQ_F32 and PVQ_BF16 (a value whose rounding to a code left float32's range is infinite), one
+ * rounding to nearest in PVQ_F16. */
+int pvq_fp8_decode(const uint8_t *codes, const uint8_t *exponents, int64_t rows, int64_t cols, void *Y, int out_dtype, int64_t ldy,
+                   void *stream);
+
+/*
+ * Y = A B^T, A [m][k] and B [n][k] in blocks, Y [m][ldy] of out_dtype: tokens times weights, any number of tokens.
+ * Sums are float32.  To PVQ_F32 they are formed of the decoded values by the bfloat16 matrix instructions; to PVQ_BF16 and PVQ_F16
+ * by the 8-bit ones, which align the products of a group of eight to the largest among them and drop what lies 14 bits below
+ * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 64) take the
+ * bfloat16 instructions for every type.  The order of the sums depends on the shape alone.
+ *   work   device, 16-byte aligned scratch of pvq_fp8_product_work_bytes bytes (may be NULL where that is 0); calls that
+ *          may overlap in time need one each
+ * k == 0 gives zeros.
+ */
+int pvq_fp8_product_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_product(const uint8_t *a_codes, const uint8_t *a_exponents, int64_t m, const uint8_t *b_codes,
+                    const uint8_t *b_exponents, int64_t n, int64_t k, void *Y, int out_dtype, int64_t ldy, void *work,
+                    size_t work_bytes, void *stream);
+
+/*
+ * The gradients of Y = X W^T, X [m][k] and W [n][k] in blocks, from dY (device, bfloat16 [m][lddy]):
+ *   pvq_fp8_input_grad    dX = dY W    [m][lddx] of out_dtype
+ *   pvq_fp8_weight_grad   dW = dY^T X  [n][lddw] of out_dtype
+ * On the bfloat16 matrix instructions, the blocks decoded exactly, sums in float32 and one rounding to out_dtype.
+ * work as for pvq_fp8_product.
+ */
+int pvq_fp8_input_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const uint8_t *w_codes, const uint8_t *w_exponents, int64_t n,
+                       int64_t k, void *dX, int out_dtype, int64_t lddx, void *work, size_t work_bytes, void *stream);
+int pvq_fp8_weight_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int64_t n, const uint8_t *x_codes, const uint8_t *x_exponents,
+                        int64_t k, void *dW, int out_dtype, int64_t lddw, void *work, size_t work_bytes, void *stream);
+
+/*
+ * The first half of a gated feed-forward block in one kernel: H = act(G) * U, G = X Wg^T, U = X Wu^T, with X [m][k],
+ * Wg and Wu [n][k] in blocks; G and U stay in registers, in float32.
+ *   PVQ_SILU  act(g) = g / (1 + exp(-g))
+ *   PVQ_GELU  act(g) = 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ *   H                    device, [m][ldh] of out_dtype, or NULL
+ *   h_codes, h_exponents H in blocks (the input of the product behind it), or NULL both; one of H and these is wanted
+ *   g_codes .. u_exponents   G and U in blocks, what the backward pass needs of them, or NULL all four
+ * Sums as in pvq_fp8_product, by the type of H (the 8-bit instructions where there is none), with G and U kept those of PVQ_F32.
+ */
+typedef enum { PVQ_SILU = 0, PVQ_GELU = 1 } pvq_activation;
+int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m, const uint8_t *gate_codes,
+                  const uint8_t *gate_exponents, const uint8_t *up_codes, const uint8_t *up_exponents, int64_t n, int64_t k,
+                  int activation, void *H, int out_dtype, int64_t ldh, uint8_t *h_codes, uint8_t *h_exponents, uint8_t *g_codes,
+                  uint8_t *g_exponents, uint8_t *u_codes, uint8_t *u_exponents, void *stream);
+
+/*
+ * Its backward pass, from dH (device, bfloat16 [m][lddh]), the block's inputs and the kept G and U:
+ *   dU = dH * act(G),  dG = dH * U * act'(G)   (float32, rounded once to bfloat16 for the matrix instructions)
+ *   dX = dG Wg + dU Wu  [m][lddx],   dWg = dG^T X  [n][lddw],   dWu = dU^T X  [n][lddw]   of out_dtype
+ * dX may be NULL, or dWg and dWu both (what is not wanted is not computed).
+ *   work   device, 16-byte aligned scratch of pvq_fp8_gated_backward_work_bytes bytes
+ */
+int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m,
+                           const uint8_t *gate_codes, const uint8_t *gate_exponents, const uint8_t *up_codes,
+                           const uint8_t *up_exponents, int64_t n, int64_t k, const uint8_t *g_codes, const uint8_t *g_exponents,
+                           const uint8_t *u_codes, const uint8_t *u_exponents, int activation, void *dX, int64_t lddx, void *dWg,
+                           void *dWu, int64_t lddw, int out_dtype, void *work, size_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,9 @@ EXPORTS = [
     "pvq_size_table_device", "pvq_hadamard",
     "pvq_ctx_create", "pvq_ctx_destroy", "pvq_ctx_info", "pvq_ctx_set_amplitude", "pvq_packed_sizes",
     "pvq_encode", "pvq_decode", "pvq_decode_gemv",
+    "pvq_fp8_sizes", "pvq_fp8_encode", "pvq_fp8_decode", "pvq_fp8_product_work_bytes", "pvq_fp8_product",
+    "pvq_fp8_input_grad_work_bytes", "pvq_fp8_input_grad", "pvq_fp8_weight_grad_work_bytes", "pvq_fp8_weight_grad",
+    "pvq_fp8_gated", "pvq_fp8_gated_backward_work_bytes", "pvq_fp8_gated_backward",
 ]
 
 # diagnostics declared in csrc/pvq_diagnostics.h, exported for the tests
@@ -79,6 +82,18 @@ def lib():
         L.pvq_decode.argtypes = [vp, vp, vp, vp, i64, i64, vp, i32, i64, vp]
         L.pvq_decode_gemv.argtypes = [vp, vp, vp, vp, i64, i64, vp, i32, i64, vp, i64, vp]
         L.pvq_decode_gemv_on.argtypes = [vp, vp, vp, vp, i64, i64, vp, i32, i64, vp, i64, vp, i32, i32]
+        sz = C.c_size_t
+        L.pvq_fp8_sizes.argtypes = [i64, i64, vp, vp]
+        L.pvq_fp8_encode.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+        L.pvq_fp8_decode.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+        for name in ("product", "input_grad", "weight_grad", "gated_backward"):
+            getattr(L, f"pvq_fp8_{name}_work_bytes").argtypes = [i64, i64, i64, i32, vp]
+        L.pvq_fp8_product.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
+        L.pvq_fp8_input_grad.argtypes = [vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
+        L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp, sz, vp]
+        L.pvq_fp8_gated.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.pvq_fp8_gated_backward.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, i64,
+                                             i32, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -401,3 +416,97 @@ def pvq_decode_gemv_on(ctx: PvqContext, packed: Packed, x, decoder: str, tile_ro
                                     packed.cols, _ptr(x), batch, ldx, _ptr(out), ldy, _stream_ptr(),
                                     {"table": 1, "walk": 2}[decoder], tile_rows), "pvq_decode_gemv_on")
     return out
+
+
+# ------------------------------------------------------------------ 8-bit blocks (torch tensors)
+
+
+class Fp8Blocks:
+    """A matrix in 8-bit blocks: codes uint8 [rows][128 ceil(cols/128)] (e4m3) and exponents uint8 [rows][4 ceil(cols/512)], a
+    power of two 2^(e - 127) for every 128 columns of a row (device tensors)."""
+
+    __slots__ = ("rows", "cols", "codes", "exponents")
+
+    def __init__(self, rows, cols, codes, exponents):
+        self.rows, self.cols, self.codes, self.exponents = rows, cols, codes, exponents
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def pvq_fp8_encode(X, out: Fp8Blocks = None) -> Fp8Blocks:
+    """The matrix X (float32, float16 or bfloat16 device tensor with unit column stride) in 8-bit blocks: activations in front of
+    a product or kept for a backward pass, decoded weights for products with many rows."""
+    native = _native_module or _native()
+    rows, cols = X.shape
+    if out is None:
+        return Fp8Blocks(rows, cols, *_result(native.fp8_encode(X, None, None), "pvq_fp8_encode"))
+    if (out.rows, out.cols) != (rows, cols):
+        raise ValueError("out is of another shape")
+    _result(native.fp8_encode(X, out.codes, out.exponents), "pvq_fp8_encode")
+    return out
+
+
+def pvq_fp8_decode(blocks: Fp8Blocks, out_dtype=None, out=None):
+    """The values of 8-bit blocks as a tensor of out_dtype (float32, float16 or bfloat16)."""
+    return _result((_native_module or _native()).fp8_decode(blocks.codes, blocks.exponents, blocks.rows, blocks.cols, out_dtype, out),
+                   "pvq_fp8_decode")
+
+
+def _same_columns(a: Fp8Blocks, b: Fp8Blocks):
+    if a.cols != b.cols:
+        raise ValueError(f"{a.cols} and {b.cols} columns")
+
+
+def pvq_fp8_product(A: Fp8Blocks, B: Fp8Blocks, out_dtype=None, out=None):
+    """A B^T of two matrices in 8-bit blocks (tokens and weights), [A.rows][B.rows] of out_dtype (float32, float16 or bfloat16)."""
+    _same_columns(A, B)
+    return _result((_native_module or _native()).fp8_product(A.codes, A.exponents, B.codes, B.exponents, A.rows, B.rows, A.cols,
+                                                             out_dtype, out), "pvq_fp8_product")
+
+
+def pvq_fp8_input_grad(dY, W: Fp8Blocks, out_dtype=None, out=None):
+    """dX = dY W, the gradient of pvq_fp8_product(X, W) with respect to X.  dY: bfloat16 [tokens][W.rows] device tensor."""
+    return _result((_native_module or _native()).fp8_input_grad(dY, W.codes, W.exponents, dY.shape[0], W.rows, W.cols, out_dtype, out),
+                   "pvq_fp8_input_grad")
+
+
+def pvq_fp8_weight_grad(dY, X: Fp8Blocks, out_dtype=None, out=None):
+    """dW = dY^T X, the gradient of pvq_fp8_product(X, W) with respect to W, from the blocks that X was multiplied or kept as.
+    dY: bfloat16 [X.rows][outputs] device tensor."""
+    return _result((_native_module or _native()).fp8_weight_grad(dY, X.codes, X.exponents, X.rows, dY.shape[1], X.cols, out_dtype, out),
+                   "pvq_fp8_weight_grad")
+
+
+def pvq_fp8_gated(X: Fp8Blocks, gate: Fp8Blocks, up: Fp8Blocks, activation: str = "silu", out_dtype=None, out=None, keep: bool = False,
+                  encode: bool = False):
+    """H = activation(X gate^T) * (X up^T) in one kernel; activation "silu" or "gelu" (its tanh form).  H is a tensor of out_dtype, or
+    with encode=True in 8-bit blocks, as the product behind it takes it.  keep=True: (H, G, U) with the two products in 8-bit
+    blocks, which pvq_fp8_gated_backward takes."""
+    _same_columns(X, gate)
+    _same_columns(X, up)
+    if gate.rows != up.rows:
+        raise ValueError(f"{gate.rows} and {up.rows} hidden units")
+    if encode and (out is not None or out_dtype is not None):
+        raise ValueError("encode=True makes new 8-bit blocks")
+    m, n = X.rows, gate.rows
+    r = _result((_native_module or _native()).fp8_gated(X.codes, X.exponents, gate.codes, gate.exponents, up.codes, up.exponents, m, n, X.cols,
+                                                        ACTIVATIONS[activation], out_dtype, out, encode, keep), "pvq_fp8_gated")
+    h, kept = (r[0], r[1:]) if keep else (r, ())
+    if encode:
+        h = Fp8Blocks(m, n, *h)
+    return (h, *(Fp8Blocks(m, n, *p) for p in kept)) if keep else h
+
+
+def pvq_fp8_gated_backward(dH, X: Fp8Blocks, gate: Fp8Blocks, up: Fp8Blocks, G: Fp8Blocks, U: Fp8Blocks, activation: str = "silu",
+                           out_dtype=None, input_grad: bool = True, weight_grads: bool = True):
+    """(dX, dgate, dup) of pvq_fp8_gated, of out_dtype, from dH (bfloat16 [X.rows][gate.rows] device tensor) and the kept G and U;
+    None for those not wanted."""
+    _same_columns(X, gate)
+    _same_columns(X, up)
+    _same_columns(G, U)
+    if not input_grad and not weight_grads:
+        return None, None, None
+    return _result((_native_module or _native()).fp8_gated_backward(
+        dH, X.codes, X.exponents, gate.codes, gate.exponents, up.codes, up.exponents, G.codes, G.exponents, U.codes, U.exponents,
+        X.rows, gate.rows, X.cols, ACTIVATIONS[activation], out_dtype, input_grad, weight_grads), "pvq_fp8_gated_backward")

@@ -1,0 +1,91 @@
+// 8-bit block matrices: the interface between the checks of arguments (pvq_fp8_host.cpp) and the kernels
+// (pvq_fp8_blocks.hip, pvq_fp8_product.hip, pvq_fp8_rows.hip, pvq_fp8_grad.hip).  Not installed; the contract is include/pvq.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <stdint.h>
+
+#include "pvq.h"
+
+// remembers the HIP error of a call for pvq_last_hip_error and returns PVQ_E_HIP (pvq_host.cpp)
+int pvq_hip_fail(hipError_t e);
+
+constexpr int kFp8Block = 128;        // values of one exponent
+
+// A block matrix [rows][cols]: a row of codes takes whole blocks, a row of exponents whole words.
+struct fp8_blocks {
+    const uint8_t *codes = nullptr, *exps = nullptr;
+    int64_t rows = 0, cols = 0;
+#if defined(__HIPCC__)
+    __host__ __device__
+#endif
+    int64_t blocks() const { return (cols + kFp8Block - 1) / kFp8Block; }
+#if defined(__HIPCC__)
+    __host__ __device__
+#endif
+    int64_t code_row() const { return blocks() * kFp8Block; }
+#if defined(__HIPCC__)
+    __host__ __device__
+#endif
+    int64_t exp_row() const { return (blocks() + 3) / 4 * 4; }
+};
+
+// A matrix of floats with unit column stride.
+struct fp8_matrix {
+    void *data = nullptr;
+    int dtype = PVQ_F32;
+    int64_t ld = 0;
+};
+
+// Y = A B^T.  work: float32 sums of the parts of a split (fp8_product_work), unused without one.
+struct fp8_product_args {
+    fp8_blocks a, b;
+    fp8_matrix y;
+    float *work;
+};
+size_t fp8_product_work(int64_t m, int64_t n, int64_t k, int out_dtype);
+hipError_t fp8_launch_product(const fp8_product_args &a, hipStream_t s);
+
+// H = act(X Wg^T) * (X Wu^T); h in floats (h.data) or in blocks (hc, he), and G and U in blocks where gc, ge, uc and ue are given
+struct fp8_gated_args {
+    fp8_blocks x, gate, up;
+    int act;
+    fp8_matrix h;
+    uint8_t *hc, *he, *gc, *ge, *uc, *ue;
+};
+hipError_t fp8_launch_gated(const fp8_gated_args &a, hipStream_t s);
+
+// Few rows of A (tokens): the kernels that stream B (pvq_fp8_rows.hip).  Called by the two above.
+bool fp8_rows_pay(int64_t m);
+hipError_t fp8_launch_product_rows(const fp8_product_args &a, hipStream_t s);
+hipError_t fp8_launch_gated_rows(const fp8_gated_args &a, hipStream_t s);
+
+// A bf16 matrix [rows][cols] with row stride ld.
+struct fp8_bf16 {
+    const uint16_t *data = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+};
+
+// out[p] = sum over the terms t of term(t): dX = sum_t dY_t W_t (transposed == false; one output, one or two terms) or
+// dW_p = dY_p^T X_p (transposed == true; one or two outputs of one term each)
+struct fp8_grad_args {
+    int pairs;
+    fp8_bf16 dy[2];
+    fp8_blocks b[2];
+    fp8_matrix out[2];
+    float *work;
+};
+size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int out_dtype, int pairs);
+size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int out_dtype, int pairs);
+hipError_t fp8_launch_input_grad(const fp8_grad_args &a, hipStream_t s);
+hipError_t fp8_launch_weight_grad(const fp8_grad_args &a, hipStream_t s);
+
+hipError_t fp8_launch_encode(const void *X, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes, uint8_t *exps, hipStream_t s);
+hipError_t fp8_launch_decode(const fp8_blocks &b, const fp8_matrix &y, hipStream_t s);
+// dG = dH U act'(G), dU = dH act(G) in bf16 with row strides of ld values, the columns from n to ld set to zero
+hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du,
+                                   int64_t ld, hipStream_t s);
+// the sums of a split, added in order: out = sum_p work[p], work [parts][rows][cols]
+hipError_t fp8_launch_join(const float *work, int parts, int64_t rows, int64_t cols, const fp8_matrix &out, hipStream_t s);

@@ -23,6 +23,8 @@ static int hip_fail(hipError_t e)
     return PVQ_E_HIP;
 }
 
+int pvq_hip_fail(hipError_t e) { return hip_fail(e); }
+
 extern "C" const char *pvq_strerror(int status)
 {
     switch (status) {

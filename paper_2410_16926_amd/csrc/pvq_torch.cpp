@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -234,6 +235,262 @@ PyObject *hadamard(PyObject *const *a)
     return status_or(status, out);
 }
 
+// ---- 8-bit blocks ------------------------------------------------------------------------------------
+// These calls check what they are given: all tensors on one GPU, which is made the current one for the call (its current
+// stream is used), block planes of the shapes that their matrix has, matrices of floats with unit column stride.
+
+struct blocks {
+    at::Tensor codes, exps;
+    const uint8_t *c() const { return (const uint8_t *)data(codes); }
+    const uint8_t *e() const { return (const uint8_t *)data(exps); }
+    uint8_t *c() { return (uint8_t *)data(codes); }
+    uint8_t *e() { return (uint8_t *)data(exps); }
+};
+
+int64_t code_row(int64_t cols) { return (cols + 127) / 128 * 128; }
+int64_t exp_row(int64_t cols) { return (code_row(cols) / 128 + 3) / 4 * 4; }
+
+// the first tensor's device, or an error
+at::Device gpu_of(const at::Tensor &t)
+{
+    if (!t.is_cuda()) throw bad_argument{PyExc_ValueError, "a tensor on the GPU is wanted"};
+    return t.device();
+}
+
+void check_plane(const at::Tensor &t, int64_t rows, int64_t row, at::Device device)
+{
+    if (t.device() != device) throw bad_argument{PyExc_ValueError, "tensors on one GPU are wanted"};
+    if (t.scalar_type() != at::kByte || t.dim() != 2 || t.size(0) != rows || t.size(1) != row || !t.is_contiguous())
+        throw bad_argument{PyExc_ValueError, "contiguous uint8 planes [rows][128 ceil(cols/128)] and [rows][4 ceil(cols/512)] are wanted"};
+}
+
+blocks blocks_of(PyObject *codes, PyObject *exps, int64_t rows, int64_t cols, at::Device device)
+{
+    blocks b{tensor(codes), tensor(exps)};
+    check_plane(b.codes, rows, code_row(cols), device);
+    check_plane(b.exps, rows, exp_row(cols), device);
+    return b;
+}
+
+blocks new_blocks(int64_t rows, int64_t cols, const at::Tensor &like)
+{
+    return {new_tensor({rows, code_row(cols)}, at::kByte, like), new_tensor({rows, exp_row(cols)}, at::kByte, like)};
+}
+
+PyObject *wrap(const blocks &b)
+{
+    PyObject *codes = THPVariable_Wrap(b.codes), *exps = THPVariable_Wrap(b.exps);
+    PyObject *r = codes && exps ? PyTuple_Pack(2, codes, exps) : nullptr;
+    Py_XDECREF(codes); Py_XDECREF(exps);
+    return r;
+}
+
+struct floats {
+    at::Tensor t;
+    int dtype;
+    int64_t ld;
+    void *p() const { return data(t); }
+};
+
+floats floats_of(const at::Tensor &t, int64_t rows, int64_t cols, at::Device device)
+{
+    if (t.device() != device) throw bad_argument{PyExc_ValueError, "tensors on one GPU are wanted"};
+    if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols) throw bad_argument{PyExc_ValueError, "a matrix of another shape is wanted"};
+    if (cols > 1 && rows > 0 && t.stride(1) != 1) throw bad_argument{PyExc_ValueError, "a matrix with unit column stride is wanted"};
+    if (rows > 1 && t.stride(0) < cols) throw bad_argument{PyExc_ValueError, "a matrix whose rows lie one behind the other is wanted"};
+    return {t, dtype_code(t.scalar_type()), rows > 1 ? t.stride(0) : std::max<int64_t>(cols, 1)};
+}
+
+floats bf16_of(PyObject *o, int64_t rows, int64_t cols, at::Device device)
+{
+    const floats f = floats_of(tensor(o), rows, cols, device);
+    if (f.dtype != PVQ_BF16) throw bad_argument{PyExc_ValueError, "a bfloat16 matrix is wanted"};
+    return f;
+}
+
+// the given result, or a new one
+floats result_of(PyObject *out, PyObject *out_dtype, int64_t rows, int64_t cols, const at::Tensor &like)
+{
+    return floats_of(out != Py_None ? tensor(out) : new_tensor({rows, cols}, scalar_type(out_dtype, at::kFloat), like), rows, cols, like.device());
+}
+
+// scratch memory of a call, from torch's allocator for the current stream
+struct scratch {
+    at::Tensor t;
+    size_t bytes;
+    scratch(size_t n, const at::Tensor &like) : bytes(n) { if (n) t = new_tensor({(int64_t)n}, at::kByte, like); }
+    void *p() const { return bytes ? data(t) : nullptr; }
+};
+
+// (X, codes or None, exponents or None): the two planes
+PyObject *fp8_encode(PyObject *const *a)
+{
+    const at::Tensor &X = tensor(a[0]);
+    const at::Device device = gpu_of(X);
+    if (X.dim() != 2) throw bad_argument{PyExc_ValueError, "a matrix is wanted"};
+    const int64_t rows = X.size(0), cols = X.size(1);
+    const floats x = floats_of(X, rows, cols, device);
+    const c10::DeviceGuard guard(device);
+    blocks b = a[1] != Py_None ? blocks_of(a[1], a[2], rows, cols, device) : new_blocks(rows, cols, X);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_encode(x.p(), x.dtype, rows, cols, x.ld, b.c(), b.e(), stream);
+    }
+    return status ? PyLong_FromLong(status) : wrap(b);
+}
+
+// (codes, exponents, rows, cols, out_dtype or None, out or None)
+PyObject *fp8_decode(PyObject *const *a)
+{
+    const int64_t rows = number(a[2]), cols = number(a[3]);
+    const at::Device device = gpu_of(tensor(a[0]));
+    const blocks b = blocks_of(a[0], a[1], rows, cols, device);
+    const c10::DeviceGuard guard(device);
+    const floats y = result_of(a[5], a[4], rows, cols, b.codes);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_decode(b.c(), b.e(), rows, cols, y.p(), y.dtype, y.ld, stream);
+    }
+    return status_or(status, y.t);
+}
+
+// (codes and exponents of A, of B, m, n, k, out_dtype or None, out or None)
+PyObject *fp8_product(PyObject *const *a)
+{
+    const int64_t m = number(a[4]), n = number(a[5]), k = number(a[6]);
+    const at::Device device = gpu_of(tensor(a[0]));
+    const blocks x = blocks_of(a[0], a[1], m, k, device), w = blocks_of(a[2], a[3], n, k, device);
+    const c10::DeviceGuard guard(device);
+    const floats y = result_of(a[8], a[7], m, n, x.codes);
+    size_t bytes = 0;
+    if (const int status = pvq_fp8_product_work_bytes(m, n, k, y.dtype, &bytes)) return PyLong_FromLong(status);
+    const scratch work(bytes, x.codes);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_product(x.c(), x.e(), m, w.c(), w.e(), n, k, y.p(), y.dtype, y.ld, work.p(), bytes, stream);
+    }
+    return status_or(status, y.t);
+}
+
+// (dY, codes and exponents of W, m, n, k, out_dtype or None, out or None)
+PyObject *fp8_input_grad(PyObject *const *a)
+{
+    const int64_t m = number(a[3]), n = number(a[4]), k = number(a[5]);
+    const at::Device device = gpu_of(tensor(a[0]));
+    const floats dy = bf16_of(a[0], m, n, device);
+    const blocks w = blocks_of(a[1], a[2], n, k, device);
+    const c10::DeviceGuard guard(device);
+    const floats dx = result_of(a[7], a[6], m, k, w.codes);
+    size_t bytes = 0;
+    if (const int status = pvq_fp8_input_grad_work_bytes(m, n, k, dx.dtype, &bytes)) return PyLong_FromLong(status);
+    const scratch work(bytes, w.codes);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_input_grad(dy.p(), dy.ld, m, w.c(), w.e(), n, k, dx.p(), dx.dtype, dx.ld, work.p(), bytes, stream);
+    }
+    return status_or(status, dx.t);
+}
+
+// (dY, codes and exponents of X, m, n, k, out_dtype or None, out or None)
+PyObject *fp8_weight_grad(PyObject *const *a)
+{
+    const int64_t m = number(a[3]), n = number(a[4]), k = number(a[5]);
+    const at::Device device = gpu_of(tensor(a[0]));
+    const floats dy = bf16_of(a[0], m, n, device);
+    const blocks x = blocks_of(a[1], a[2], m, k, device);
+    const c10::DeviceGuard guard(device);
+    const floats dw = result_of(a[7], a[6], n, k, x.codes);
+    size_t bytes = 0;
+    if (const int status = pvq_fp8_weight_grad_work_bytes(m, n, k, dw.dtype, &bytes)) return PyLong_FromLong(status);
+    const scratch work(bytes, x.codes);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_weight_grad(dy.p(), dy.ld, m, n, x.c(), x.e(), k, dw.p(), dw.dtype, dw.ld, work.p(), bytes, stream);
+    }
+    return status_or(status, dw.t);
+}
+
+// (codes and exponents of X, gate, up, m, n, k, activation, out_dtype or None, out or None, whether H is wanted in blocks, whether
+// G and U are kept): H (a tensor, or the two planes), or (H, G's planes, U's planes)
+PyObject *fp8_gated(PyObject *const *a)
+{
+    const int64_t m = number(a[6]), n = number(a[7]), k = number(a[8]);
+    const int act = (int)number(a[9]);
+    const bool encoded = PyObject_IsTrue(a[12]) == 1, keep = PyObject_IsTrue(a[13]) == 1;
+    const at::Device device = gpu_of(tensor(a[0]));
+    const blocks x = blocks_of(a[0], a[1], m, k, device), gate = blocks_of(a[2], a[3], n, k, device), up = blocks_of(a[4], a[5], n, k, device);
+    const c10::DeviceGuard guard(device);
+    floats h{{}, PVQ_BF16, 0};
+    blocks hb, g, u;
+    if (encoded) hb = new_blocks(m, n, x.codes);
+    else h = result_of(a[11], a[10], m, n, x.codes);
+    if (keep) { g = new_blocks(m, n, x.codes); u = new_blocks(m, n, x.codes); }
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_gated(x.c(), x.e(), m, gate.c(), gate.e(), up.c(), up.e(), n, k, act, encoded ? nullptr : h.p(), h.dtype, h.ld,
+                               encoded ? hb.c() : nullptr, encoded ? hb.e() : nullptr, keep ? g.c() : nullptr, keep ? g.e() : nullptr,
+                               keep ? u.c() : nullptr, keep ? u.e() : nullptr, stream);
+    }
+    if (status) return PyLong_FromLong(status);
+    PyObject *first = encoded ? wrap(hb) : THPVariable_Wrap(h.t);
+    if (!keep || !first) return first;
+    PyObject *second = wrap(g), *third = wrap(u);
+    PyObject *r = second && third ? PyTuple_Pack(3, first, second, third) : nullptr;
+    Py_DECREF(first); Py_XDECREF(second); Py_XDECREF(third);
+    return r;
+}
+
+// (dH, codes and exponents of X, gate, up, G, U, m, n, k, activation, out_dtype or None, whether dX is wanted, whether dWg and dWu
+// are): (dX or None, dWg or None, dWu or None)
+PyObject *fp8_gated_backward(PyObject *const *a)
+{
+    const int64_t m = number(a[11]), n = number(a[12]), k = number(a[13]);
+    const int act = (int)number(a[14]);
+    const bool want_x = PyObject_IsTrue(a[16]) == 1, want_w = PyObject_IsTrue(a[17]) == 1;
+    const at::Device device = gpu_of(tensor(a[0]));
+    const floats dh = bf16_of(a[0], m, n, device);
+    const blocks x = blocks_of(a[1], a[2], m, k, device), gate = blocks_of(a[3], a[4], n, k, device), up = blocks_of(a[5], a[6], n, k, device);
+    const blocks g = blocks_of(a[7], a[8], m, n, device), u = blocks_of(a[9], a[10], m, n, device);
+    const c10::DeviceGuard guard(device);
+    const at::ScalarType type = scalar_type(a[15], at::kFloat);
+    const int dtype = dtype_code(type);
+    at::Tensor dx, dwg, dwu;
+    if (want_x) dx = new_tensor({m, k}, type, x.codes);
+    if (want_w) { dwg = new_tensor({n, k}, type, x.codes); dwu = new_tensor({n, k}, type, x.codes); }
+    size_t bytes = 0;
+    if (const int status = pvq_fp8_gated_backward_work_bytes(m, n, k, dtype, &bytes)) return PyLong_FromLong(status);
+    const scratch work(bytes, x.codes);
+    void *stream = current_stream();
+    int status;
+    {
+        without_lock unlocked;
+        status = pvq_fp8_gated_backward(dh.p(), dh.ld, x.c(), x.e(), m, gate.c(), gate.e(), up.c(), up.e(), n, k, g.c(), g.e(), u.c(), u.e(), act,
+                                        want_x ? data(dx) : nullptr, k, want_w ? data(dwg) : nullptr, want_w ? data(dwu) : nullptr, k, dtype,
+                                        work.p(), bytes, stream);
+    }
+    if (status) return PyLong_FromLong(status);
+    PyObject *r = PyTuple_New(3);
+    const at::Tensor *parts[3] = {want_x ? &dx : nullptr, want_w ? &dwg : nullptr, want_w ? &dwu : nullptr};
+    for (int i = 0; r && i < 3; i++) {
+        PyObject *o = parts[i] ? THPVariable_Wrap(*parts[i]) : Py_NewRef(Py_None);
+        if (!o) { Py_CLEAR(r); break; }
+        PyTuple_SET_ITEM(r, i, o);
+    }
+    return r;
+}
+
 // (): the current stream's handle
 PyObject *stream(PyObject *const *) { return PyLong_FromVoidPtr(current_stream()); }
 
@@ -255,7 +512,9 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define PVQ_METHOD(NAME, N) {#NAME, (PyCFunction)(void (*)(void))call<NAME, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PVQ_METHOD(encode, 6), PVQ_METHOD(rotate_encode, 7), PVQ_METHOD(decode, 8), PVQ_METHOD(decode_gemv, 8),
-                         PVQ_METHOD(hadamard, 6), PVQ_METHOD(stream, 0), {nullptr, nullptr, 0, nullptr}};
+                         PVQ_METHOD(hadamard, 6), PVQ_METHOD(stream, 0), PVQ_METHOD(fp8_encode, 3), PVQ_METHOD(fp8_decode, 6),
+                         PVQ_METHOD(fp8_product, 9), PVQ_METHOD(fp8_input_grad, 8), PVQ_METHOD(fp8_weight_grad, 8),
+                         PVQ_METHOD(fp8_gated, 14), PVQ_METHOD(fp8_gated_backward, 18), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pvq_torch", "libpvq's calls on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
