@@ -91,6 +91,35 @@ __device__ inline void store4(const fp8_matrix &y, int64_t row, int64_t col, int
     for (int i = 0; i < 4; i++) if (i < count) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
 }
 
+// The same of two fragments side by side (columns col .. and col + 16 .., a lane's four at 4 quarter of each): lanes of quarters 2 p and
+// 2 p + 1 exchange halves, so that each holds eight neighbouring columns, of the left fragment or the right one.  A row's store is
+// 64 bytes in a row in place of 32.  Only for what lies inside, in rows aligned to eight values; `col` is that of the left fragment.
+__device__ inline void store_pair(const fp8_matrix &y, int64_t row, int64_t col, int quarter, f32x4 left, f32x4 right)
+{
+    const int64_t at = row * y.ld + col + 16 * (quarter & 1) + 8 * (quarter >> 1);
+    if (y.dtype == PVQ_F32) {
+        u32x4 lo, hi;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(left[i]), __float_as_uint(right[i]), false, false);
+            lo[i] = r[0]; hi[i] = r[1];
+        }
+        u32x4 *p = reinterpret_cast<u32x4 *>(reinterpret_cast<float *>(y.data) + at);
+        p[0] = lo; p[1] = hi;
+        return;
+    }
+    const bool b = y.dtype == PVQ_BF16;
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const uint32_t l = b ? bf16_pair(left[2 * i], left[2 * i + 1]) : f16_pair(left[2 * i], left[2 * i + 1]);
+        const uint32_t r = b ? bf16_pair(right[2 * i], right[2 * i + 1]) : f16_pair(right[2 * i], right[2 * i + 1]);
+        const auto s = __builtin_amdgcn_permlane16_swap(l, r, false, false);
+        w[i] = s[0]; w[2 + i] = s[1];
+    }
+    *reinterpret_cast<u32x4 *>(reinterpret_cast<uint16_t *>(y.data) + at) = w;
+}
+
 // Activations.  sigma(x) = 1 / (1 + exp(-x)) by the hardware's 2^x and reciprocal, each off by about one place; exp(-x) may be
 // infinite, sigma is 0 then.  silu(g) = g sigma(g); gelu in its tanh form, 0.5 g (1 + tanh w) = g sigma(2 w) with
 // w = sqrt(2/pi) (g + 0.044715 g^3), of which nothing changes beyond |g| = 16 but the factor g.
