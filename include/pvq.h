@@ -319,7 +319,7 @@ int pvq_decode_gemv(const pvq_ctx *ctx, const uint32_t *index, const void *scale
  * instruction multiplies them in by itself, and because every decoded value is then exact in bfloat16.
  *
  * Everywhere below: codes 16-byte aligned, exponents 4-byte aligned; matrices of floats aligned to their element, any ld >= cols
- * (rows that are aligned to 16 bytes are faster); rows or cols may be 0; columns of a block matrix at most 4194304 (2^22),
+ * (rows that are aligned to 16 bytes are faster, and are read to the end of their last 16 bytes); rows or cols may be 0; columns of a block matrix at most 4194304 (2^22),
  * rows at most 2^30 and values 2^41, else PVQ_E_UNSUPPORTED.
  * Calls are asynchronous, launch kernels on `stream` only and may be captured.  NaN codes give NaN; codes behind the last
  * column that are not zero and exponent bytes outside 17 .. 247 (which encoding never writes) give unspecified values, never

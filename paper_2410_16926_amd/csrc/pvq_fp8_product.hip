@@ -1,5 +1,5 @@
 // Products of 8-bit block matrices in tiles: Y = A B^T, and the gated block H = act(X Wg^T) * (X Wu^T).
-#include "pvq_fp8_dev.h"
+#include "pvq_fp8_tile.h"
 
 #include <type_traits>
 
@@ -17,62 +17,6 @@ __device__ inline f32x4 multiply_codes(i32x8 a, uint32_t ea, i32x8 b, uint32_t e
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)ea, 0, (int)eb);
 }
-
-// The same with sums in accumulation registers, which hold nothing else then (left to the compiler, sums of 256 registers beside operands of 192
-// move between the two halves of the register file in the loop), and byte AT of words of four exponents.  A result is read by hand, at
-// least 8 passes of 4 cycles later.
-template <int AT>
-__device__ inline void multiply_accumulated(f32x4 &c, i32x8 a, uint32_t ea, i32x8 b, uint32_t eb)
-{
-    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%5,0] op_sel_hi:[%6,%6,0]"
-                 : "+a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(AT & 1), "n"(AT >> 1));
-}
-
-// ---- loads into LDS --------------------------------------------------------------------------------------------------
-// 1 KiB a wave: lane i's 16 bytes from `base` + `offset` to `lds` + 16 i.  The compiler does not count these loads: they are
-// waited for by hand (all_loads) in front of the barrier behind which they are read.
-__device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
-}
-__device__ inline void load_words_to_lds(const void *base, uint32_t offset, uint32_t lds)     // 4 bytes a lane
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
-}
-// The same from a buffer of `bytes` bytes (below 4 GiB), base, size and `uniform` in scalar registers: nothing is fetched from behind its end.
-typedef __attribute__((ext_vector_type(4))) uint32_t buffer_t;
-__device__ inline buffer_t make_buffer(const void *base, int64_t bytes)
-{
-    const uint64_t p = (uint64_t)base;
-    return buffer_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFFu,
-                    (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes), 0x00020000u};
-}
-__device__ inline void load_to_lds(buffer_t from, uint32_t offset, uint32_t uniform, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
-}
-__device__ inline void load_words_to_lds(buffer_t from, uint32_t offset, uint32_t uniform, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
-}
-__device__ inline void all_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
-
-// all but the last N
-template <int N>
-__device__ inline void loads_but() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
-// what a wave has read from LDS is in its registers
-__device__ inline void all_reads() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
-// (matrix instructions touch no memory: nothing but the scheduling barriers keeps them on their side)
-__device__ inline void barrier()
-{
-    asm volatile("" : : : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" : : : "memory");
-}
-
-__device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
 // A tile row is a block of codes, 128 bytes in eight chunks; chunk c of row r lies at place c ^ (r / 2 % 8), so that
 // what sixteen lanes read at one chunk number of sixteen rows lies in all 64 banks.
@@ -95,21 +39,9 @@ struct tile_args {
     int vec;                     // what y's rows are aligned to: 8 values, 4 or 1
 };
 
-// Tiles of the result in bands of 8 rows of tiles, down a band's columns one after the other: the workgroups of a chiplet
-// at work at one time share few rows of A and B in its L2.
-__device__ inline void tile_of(const tile_args &t, int id, int &tm, int &tn)
-{
-    constexpr int kBand = 8;
-    const int per = kBand * t.tiles_n, band = id / per, rows = min(kBand, t.tiles_m - band * kBand), in = id - band * per;
-    // (in scalar registers, as are the addresses that follow from them)
-    tm = __builtin_amdgcn_readfirstlane(band * kBand + in % rows);
-    tn = __builtin_amdgcn_readfirstlane(in / rows);
-}
-
 // The tile's sums, or what the gated block makes of them, to memory.  A lane has four neighbouring columns of one row: columns 4 quarter .. of
 // a fragment, row lane % 16.
-// ACCUMULATION: the sums are in accumulation registers and are to stay there but for those at work (moved where the compiler likes, they would
-// take the loop's registers).
+// ACCUMULATION: the sums are in accumulation registers.
 template <int TM, int TN, int WM, int WN, bool GATED, bool ACCUMULATION>
 __device__ inline void store_tile(const tile_args &t, uint8_t *lds, f32x4 (&acc)[TM / WM / 16][TN / WN / 16], int tm, int tn, int part)
 {
@@ -124,15 +56,8 @@ __device__ inline void store_tile(const tile_args &t, uint8_t *lds, f32x4 (&acc)
     const int64_t col0 = n0 + wn * FH * 16;
     // (what the gated block makes is formed where it is wanted, twice for blocks: all of it at once would not fit beside the sums)
     auto sum = [&](int i, int j) {
-        if constexpr (!ACCUMULATION) return acc[i][j];
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            float x;
-            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[i][j][e]));
-            v[e] = x;
-        }
-        return v;
+        if constexpr (ACCUMULATION) return read_sums(acc[i][j]);
+        else return acc[i][j];
     };
     auto result = [&](int i, int j) {
         f32x4 v = sum(i, j);
@@ -144,25 +69,7 @@ __device__ inline void store_tile(const tile_args &t, uint8_t *lds, f32x4 (&acc)
         return v;
     };
     const int vec = !GATED && t.parts > 1 ? (t.n % 8 == 0 ? 8 : t.n % 4 == 0 ? 4 : 1) : t.vec;
-    if (y.data && vec == 8 && m0 + TM <= rows && n0 + kCols <= t.n) {
-#pragma unroll
-        for (int i = 0; i < FM; i++)
-#pragma unroll
-            for (int j = 0; j < FH; j += 2) store_pair(y, m0 + wm * FM * 16 + i * 16 + r16, col0 + j * 16, quarter, result(i, j), result(i, j + 1));
-    } else if (y.data) {
-#pragma unroll
-        for (int i = 0; i < FM; i++) {
-            const int64_t row = m0 + wm * FM * 16 + i * 16 + r16;
-#pragma unroll
-            for (int j = 0; j < FH; j++) {
-                const int64_t col = col0 + j * 16 + 4 * quarter;
-                const f32x4 v = result(i, j);
-                if (row >= rows) continue;
-                if (vec >= 4) store4<true>(y, row, col, t.n - col, v);
-                else store4<false>(y, row, col, t.n - col, v);
-            }
-        }
-    }
+    if (y.data) store_fragments<FM, FH>(y, vec, rows, t.n, m0 + wm * FM * 16, col0, result);
     if constexpr (GATED) {
         // to blocks: the tile's hidden units are one block, of which the WN waves of a row of tiles hold a part each
         if constexpr (kCols == kFp8Block) {
@@ -233,7 +140,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void tile_kernel(tile_args t)
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16, group = wave / (kWaves / 2);
     int tm, tn;
-    tile_of(t, chiplet_order(blockIdx.x, gridDim.x), tm, tn);
+    tile_of(t.tiles_m, t.tiles_n, chiplet_order(blockIdx.x, gridDim.x), tm, tn);
     const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * kCols;
     const int part = blockIdx.y;
     const int kb0 = part * t.blocks_a_part, kb1 = min(kb0 + t.blocks_a_part, (int)t.a.blocks());
@@ -415,7 +322,7 @@ __global__ __launch_bounds__(256) void big_tile_kernel(tile_args t)
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / 2, wn = wave % 2, r16 = lane % 16, quarter = lane / 16;
     int tm, tn;
-    tile_of(t, chiplet_order(blockIdx.x, gridDim.x), tm, tn);
+    tile_of(t.tiles_m, t.tiles_n, chiplet_order(blockIdx.x, gridDim.x), tm, tn);
     const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kCols;
     const int part = blockIdx.y;
     const int kb0 = part * t.blocks_a_part, kb1 = min(kb0 + t.blocks_a_part, (int)t.a.blocks());       // (kb0 a multiple of four)
@@ -543,9 +450,7 @@ __global__ __launch_bounds__(256) void big_tile_kernel(tile_args t)
         }
         all_loads();
     }
-    // the last matrix instruction's result is there before it is read (store_tile reads by hand): 8 passes of 4 cycles, and some
-    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" : : : "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    sums_are_there();
     store_tile<kTile, kTile, 2, 2, GATED, true>(t, lds, acc, tm, tn, part);
 }
 
@@ -576,14 +481,6 @@ hipError_t launch_tile(tile_args &t, hipStream_t s)
     t.blocks_a_part = (int)((t.a.blocks() + t.parts - 1) / t.parts);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(t.tiles_m * t.tiles_n), (unsigned)t.parts), dim3(WM * WN * kWave), kLds, s, t);
     return hipGetLastError();
-}
-
-int row_alignment(const fp8_matrix &y)
-{
-    const int size = y.dtype == PVQ_F32 ? 4 : 2;
-    for (const int n : {8, 4})
-        if ((uintptr_t)y.data % std::min(16, n * size) == 0 && y.ld % n == 0) return n;
-    return 1;
 }
 
 }  // namespace
