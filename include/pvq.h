@@ -363,12 +363,13 @@ int pvq_fp8_product(const uint8_t *a_codes, const uint8_t *a_exponents, int64_t 
  *   pvq_fp8_input_grad    dX = dY W    [m][lddx] of out_dtype
  *   pvq_fp8_weight_grad   dW = dY^T X  [n][lddw] of out_dtype
  * On the bfloat16 matrix instructions, the blocks decoded exactly, sums in float32 and one rounding to out_dtype.
- * work as for pvq_fp8_product.
+ * work as for pvq_fp8_product; its size depends on dY and lddy by their alignment alone (rows that do not start at 16 bytes are copied
+ * there first).
  */
-int pvq_fp8_input_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const uint8_t *w_codes, const uint8_t *w_exponents, int64_t n,
                        int64_t k, void *dX, int out_dtype, int64_t lddx, void *work, size_t work_bytes, void *stream);
-int pvq_fp8_weight_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_weight_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int64_t n, const uint8_t *x_codes, const uint8_t *x_exponents,
                         int64_t k, void *dW, int out_dtype, int64_t lddw, void *work, size_t work_bytes, void *stream);
 
@@ -381,12 +382,14 @@ int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int64_t n, cons
  *   h_codes, h_exponents H in blocks (the input of the product behind it), or NULL both; one of H and these is wanted
  *   g_codes .. u_exponents   G and U in blocks, what the backward pass needs of them, or NULL all four
  * Sums as in pvq_fp8_product, by the type of H (the 8-bit instructions where there is none), with G and U kept those of PVQ_F32.
+ *   work                 as for pvq_fp8_product; to_blocks: not zero where H is wanted in blocks or G and U are kept
  */
 typedef enum { PVQ_SILU = 0, PVQ_GELU = 1 } pvq_activation;
+int pvq_fp8_gated_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, int to_blocks, size_t *bytes);
 int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m, const uint8_t *gate_codes,
                   const uint8_t *gate_exponents, const uint8_t *up_codes, const uint8_t *up_exponents, int64_t n, int64_t k,
                   int activation, void *H, int out_dtype, int64_t ldh, uint8_t *h_codes, uint8_t *h_exponents, uint8_t *g_codes,
-                  uint8_t *g_exponents, uint8_t *u_codes, uint8_t *u_exponents, void *stream);
+                  uint8_t *g_exponents, uint8_t *u_codes, uint8_t *u_exponents, void *work, size_t work_bytes, void *stream);
 
 /*
  * Its backward pass, from dH (device, bfloat16 [m][lddh]), the block's inputs and the kept G and U:
@@ -395,7 +398,7 @@ int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m,
  * dX may be NULL, or dWg and dWu both (what is not wanted is not computed).
  *   work   device, 16-byte aligned scratch of pvq_fp8_gated_backward_work_bytes bytes
  */
-int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes);
+int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m,
                            const uint8_t *gate_codes, const uint8_t *gate_exponents, const uint8_t *up_codes,
                            const uint8_t *up_exponents, int64_t n, int64_t k, const uint8_t *g_codes, const uint8_t *g_exponents,

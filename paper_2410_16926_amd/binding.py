@@ -21,7 +21,7 @@ EXPORTS = [
     "pvq_encode", "pvq_decode", "pvq_decode_gemv",
     "pvq_fp8_sizes", "pvq_fp8_encode", "pvq_fp8_decode", "pvq_fp8_product_work_bytes", "pvq_fp8_product",
     "pvq_fp8_input_grad_work_bytes", "pvq_fp8_input_grad", "pvq_fp8_weight_grad_work_bytes", "pvq_fp8_weight_grad",
-    "pvq_fp8_gated", "pvq_fp8_gated_backward_work_bytes", "pvq_fp8_gated_backward",
+    "pvq_fp8_gated_work_bytes", "pvq_fp8_gated", "pvq_fp8_gated_backward_work_bytes", "pvq_fp8_gated_backward",
 ]
 
 # diagnostics declared in csrc/pvq_diagnostics.h, exported for the tests
@@ -86,12 +86,14 @@ def lib():
         L.pvq_fp8_sizes.argtypes = [i64, i64, vp, vp]
         L.pvq_fp8_encode.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
         L.pvq_fp8_decode.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
-        for name in ("product", "input_grad", "weight_grad", "gated_backward"):
-            getattr(L, f"pvq_fp8_{name}_work_bytes").argtypes = [i64, i64, i64, i32, vp]
+        L.pvq_fp8_product_work_bytes.argtypes = [i64, i64, i64, i32, vp]
+        L.pvq_fp8_input_grad_work_bytes.argtypes = L.pvq_fp8_weight_grad_work_bytes.argtypes = [vp, i64, i64, i64, i64, vp]
+        L.pvq_fp8_gated_work_bytes.argtypes = [i64, i64, i64, i32, i32, vp]
+        L.pvq_fp8_gated_backward_work_bytes.argtypes = [i64, i64, i64, vp]
         L.pvq_fp8_product.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
         L.pvq_fp8_input_grad.argtypes = [vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
         L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp, sz, vp]
-        L.pvq_fp8_gated.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.pvq_fp8_gated.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.pvq_fp8_gated_backward.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, i64,
                                              i32, vp, sz, vp]
         _lib = L

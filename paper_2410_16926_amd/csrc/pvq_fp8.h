@@ -39,6 +39,22 @@ struct fp8_matrix {
     int64_t ld = 0;
 };
 
+// Into how many parts the sums of `tiles` tiles of `steps` steps are split: as many as take least, with a workgroup to a unit, 6 us around its steps,
+// and the parts' sums (values of them) written, and read again by a kernel that adds them.
+constexpr double kByteStepUs = 1.4, kWideStepUs = 1.2;       // a step of a 256 x 256 tile: 128 of the sum on the 8-bit, 64 on the bfloat16 instruction
+inline int fp8_parts(int64_t tiles, int64_t steps, double step_us, int64_t values)
+{
+    int best = 1;
+    double least = 0.0;
+    for (int parts = 1; parts <= 32 && (parts == 1 || steps >= 2 * parts); parts++) {
+        const double rounds = (double)((tiles * parts + 255) / 256);
+        double us = rounds * ((double)((steps + parts - 1) / parts) * step_us + 6.0);
+        if (parts > 1) us += 4.0 + 8.0 * parts * (double)values / 4e6;
+        if (parts == 1 || us < least) { best = parts; least = us; }
+    }
+    return best;
+}
+
 // Y = A B^T.  work: float32 sums of the parts of a split (fp8_product_work), unused without one.
 struct fp8_product_args {
     fp8_blocks a, b;
@@ -54,15 +70,20 @@ struct fp8_gated_args {
     int act;
     fp8_matrix h;
     uint8_t *hc, *he, *gc, *ge, *uc, *ue;
+    float *work;
 };
+// wide: sums on the bfloat16 instruction (float32 results, kept products)
+size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide);
 hipError_t fp8_launch_gated(const fp8_gated_args &a, hipStream_t s);
+// ... of the parts of G and U, [parts][2][rows][cols]
+hipError_t fp8_launch_gated_join(const float *work, int parts, const fp8_gated_args &a, hipStream_t s);
 
 // Few rows of A (tokens): the kernels that stream B (pvq_fp8_rows.hip).  Called by the two above.
 bool fp8_rows_pay(int64_t m);
 hipError_t fp8_launch_product_rows(const fp8_product_args &a, hipStream_t s);
 hipError_t fp8_launch_gated_rows(const fp8_gated_args &a, hipStream_t s);
 
-// A bf16 matrix [rows][cols] with row stride ld.
+// A bf16 matrix [rows][cols] with row stride ld.  (The gradient kernels take rows aligned to 16 bytes, of at most 2^22 values.)
 struct fp8_bf16 {
     const uint16_t *data = nullptr;
     int64_t rows = 0, cols = 0, ld = 0;
@@ -77,8 +98,8 @@ struct fp8_grad_args {
     fp8_matrix out[2];
     float *work;
 };
-size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int out_dtype, int pairs);
-size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int out_dtype, int pairs);
+size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
+size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
 hipError_t fp8_launch_input_grad(const fp8_grad_args &a, hipStream_t s);
 hipError_t fp8_launch_weight_grad(const fp8_grad_args &a, hipStream_t s);
 
@@ -87,5 +108,7 @@ hipError_t fp8_launch_decode(const fp8_blocks &b, const fp8_matrix &y, hipStream
 // dG = dH U act'(G), dU = dH act(G) in bf16 with row strides of ld values, the columns from n to ld set to zero
 hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du,
                                    int64_t ld, hipStream_t s);
+// a bf16 matrix to rows of `ld` values that start at 16 bytes, the columns behind the last zero
+hipError_t fp8_launch_align(const fp8_bf16 &from, uint16_t *to, int64_t ld, hipStream_t s);
 // the sums of a split, added in order: out = sum_p work[p], work [parts][rows][cols]
 hipError_t fp8_launch_join(const float *work, int parts, int64_t rows, int64_t cols, const fp8_matrix &out, hipStream_t s);

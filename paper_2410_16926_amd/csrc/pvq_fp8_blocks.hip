@@ -45,6 +45,22 @@ __device__ inline void load8(const typename element<T>::type *row, int64_t c, in
     for (int i = 0; i < 8; i++) v[i] = c + i < cols ? to_float<T>(row[c + i]) : 0.0f;
 }
 
+// A wave's item of four blocks, whose largest magnitudes are `top`: the lane's eight codes, and the blocks' exponents in one word.
+__device__ inline void store_codes(uint8_t *codes, uint8_t *exps, int64_t tile, int64_t c, int64_t code_row, int lane, const float (&v)[8], uint32_t top)
+{
+    const uint32_t e = exponent_of(top);
+    const float inverse = scale_of(254 - e);
+    if (c < code_row) {
+        const u32x2 w = {codes4(v[0], v[1], v[2], v[3], inverse), codes4(v[4], v[5], v[6], v[7], inverse)};
+        *reinterpret_cast<u32x2 *>(codes + c) = w;
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if ((tile * 4 + i) * kFp8Block < code_row) word |= (uint32_t)__builtin_amdgcn_readlane((int)e, 16 * i) << (8 * i);
+    if (lane == 0) *reinterpret_cast<uint32_t *>(exps + tile * 4) = word;
+}
+
 template <int T, bool VEC>
 __global__ __launch_bounds__(kThreads) void encode_kernel(const typename element<T>::type *X, int64_t rows, int64_t cols, int64_t ldx,
                                                           uint8_t *codes, uint8_t *exps, int64_t code_row, int64_t exp_row, int tiles)
@@ -59,17 +75,7 @@ __global__ __launch_bounds__(kThreads) void encode_kernel(const typename element
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) top = max(top, finite_bits(v[i]));
-        const uint32_t e = exponent_of(block_max(top));
-        const float inverse = scale_of(254 - e);
-        if (c < code_row) {
-            const u32x2 w = {codes4(v[0], v[1], v[2], v[3], inverse), codes4(v[4], v[5], v[6], v[7], inverse)};
-            *reinterpret_cast<u32x2 *>(codes + row * code_row + c) = w;
-        }
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            if ((tile * 4 + i) * kFp8Block < code_row) word |= (uint32_t)__builtin_amdgcn_readlane((int)e, 16 * i) << (8 * i);
-        if (lane == 0) *reinterpret_cast<uint32_t *>(exps + row * exp_row + tile * 4) = word;
+        store_codes(codes + row * code_row, exps + row * exp_row, tile, c, code_row, lane, v, block_max(top));
     }
 }
 
@@ -146,6 +152,58 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *work, int p
     store4<VEC>(out, row, c, count, sum);
 }
 
+// The parts' sums of G and U, [part][G, U][rows][cols], added, and what the gated block makes of them; a wave's items as in encode_kernel.
+template <bool VEC>
+__global__ __launch_bounds__(kThreads) void gated_join_kernel(const float *work, int parts, int64_t rows, int64_t cols, int act, fp8_matrix h,
+                                                              uint8_t *hc, uint8_t *he, uint8_t *gc, uint8_t *ge, uint8_t *uc, uint8_t *ue, int tiles)
+{
+    const int lane = threadIdx.x % kWave;
+    const int64_t items = rows * tiles, step = (int64_t)gridDim.x * kWaves, code_row = (cols + kFp8Block - 1) / kFp8Block * kFp8Block, exp_row = (int64_t)tiles * 4;
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); item < items; item += step) {
+        const int64_t row = item / tiles, tile = item - row * tiles, c = tile * kItem + 8 * lane;
+        float g[8] = {}, u[8] = {}, v[8];
+        for (int p = 0; p < parts; p++) {
+            float a[8], b[8];
+            const float *from = work + (int64_t)p * 2 * rows * cols + row * cols;
+            load8<PVQ_F32, VEC>(from, c, cols, a);
+            load8<PVQ_F32, VEC>(from + rows * cols, c, cols, b);
+#pragma unroll
+            for (int i = 0; i < 8; i++) { g[i] += a[i]; u[i] += b[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = act_value(act, g[i]) * u[i];
+        if (h.data)
+#pragma unroll
+            for (int i = 0; i < 8; i += 4)
+                if (c + i < cols) store4<false>(h, row, c + i, cols - c - i, f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]});
+        auto to_blocks = [&](uint8_t *codes, uint8_t *exps, const float (&w)[8]) {
+            if (!codes) return;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) top = max(top, finite_bits(w[i]));
+            store_codes(codes + row * code_row, exps + row * exp_row, tile, c, code_row, lane, w, block_max(top));
+        };
+        to_blocks(gc, ge, g);
+        to_blocks(uc, ue, u);
+        to_blocks(hc, he, v);
+    }
+}
+
+// a lane eight values
+__global__ __launch_bounds__(kThreads) void align_kernel(fp8_bf16 from, uint16_t *to, int64_t ld)
+{
+    const int64_t runs = ld / 8, total = from.rows * runs;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / runs, c = (i - row * runs) * 8;
+        const uint16_t *p = from.data + row * from.ld + c;
+        u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (c + e < from.cols) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+        *reinterpret_cast<u32x4 *>(to + row * ld + c) = w;
+    }
+}
+
 unsigned grid_for(int64_t work, int64_t most) { return (unsigned)std::max<int64_t>(1, std::min(work, most)); }
 
 bool aligned_rows(const void *p, int64_t ld, int size, int bytes) { return (uintptr_t)p % bytes == 0 && (ld * size) % bytes == 0; }
@@ -202,5 +260,24 @@ hipError_t fp8_launch_join(const float *work, int parts, int64_t rows, int64_t c
     const unsigned grid = (unsigned)((rows * ((cols + 3) / 4) + kThreads - 1) / kThreads);
     if (vector_rows(out)) hipLaunchKernelGGL(join_kernel<true>, dim3(grid), dim3(kThreads), 0, s, work, parts, rows, cols, out);
     else hipLaunchKernelGGL(join_kernel<false>, dim3(grid), dim3(kThreads), 0, s, work, parts, rows, cols, out);
+    return hipGetLastError();
+}
+
+hipError_t fp8_launch_gated_join(const float *work, int parts, const fp8_gated_args &a, hipStream_t s)
+{
+    const int64_t rows = a.x.rows, cols = a.gate.rows;
+    const int tiles = (int)((cols + kItem - 1) / kItem);
+    const unsigned grid = grid_for((rows * tiles + kWaves - 1) / kWaves, 256 * 8 * 4);
+    if (cols % 4 == 0)
+        hipLaunchKernelGGL(gated_join_kernel<true>, dim3(grid), dim3(kThreads), 0, s, work, parts, rows, cols, a.act, a.h, a.hc, a.he, a.gc, a.ge, a.uc, a.ue, tiles);
+    else
+        hipLaunchKernelGGL(gated_join_kernel<false>, dim3(grid), dim3(kThreads), 0, s, work, parts, rows, cols, a.act, a.h, a.hc, a.he, a.gc, a.ge, a.uc, a.ue, tiles);
+    return hipGetLastError();
+}
+
+hipError_t fp8_launch_align(const fp8_bf16 &from, uint16_t *to, int64_t ld, hipStream_t s)
+{
+    const unsigned grid = grid_for((from.rows * (ld / 8) + kThreads - 1) / kThreads, 256 * 8 * 4);
+    hipLaunchKernelGGL(align_kernel, dim3(grid), dim3(kThreads), 0, s, from, to, ld);
     return hipGetLastError();
 }

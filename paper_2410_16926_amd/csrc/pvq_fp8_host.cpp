@@ -48,10 +48,25 @@ int first_of(std::initializer_list<int> codes)
     return PVQ_OK;
 }
 
-// dY of the backward products: the row stride of a workspace's matrices, in values
+// the row stride of a workspace's bfloat16 matrices, in values
 int64_t slope_row(int64_t n) { return (n + 63) / 64 * 64; }
 
+// Whether the gradient kernels can take dY as it is: rows aligned to 16 bytes, a tile's within 32-bit offsets.  Otherwise it is copied first.
+bool whole_rows(const void *dY, int64_t ld) { return aligned(dY, 16) && ld % 8 == 0 && ld <= kMostCols; }
+
 size_t up16(size_t v) { return (v + 15) / 16 * 16; }
+
+size_t copy_bytes(const void *dY, int64_t ld, int64_t m, int64_t n) { return whole_rows(dY, ld) ? 0 : up16((size_t)m * slope_row(n) * 2); }
+
+// a gradient's dY, copied to the front of its workspace where it has to be; the split's sums behind it
+hipError_t take_dy(fp8_grad_args &a, void *work, size_t copy, hipStream_t s)
+{
+    a.work = (float *)((char *)work + copy);
+    if (copy == 0) return hipSuccess;
+    const fp8_bf16 from = a.dy[0];
+    a.dy[0] = {(const uint16_t *)work, from.rows, from.cols, slope_row(from.cols)};
+    return fp8_launch_align(from, (uint16_t *)work, a.dy[0].ld, s);
+}
 
 }  // namespace
 
@@ -110,11 +125,11 @@ extern "C" int pvq_fp8_product(const uint8_t *a_codes, const uint8_t *a_exponent
     return status_of(fp8_rows_pay(m) ? fp8_launch_product_rows(a, (hipStream_t)stream) : fp8_launch_product(a, (hipStream_t)stream));
 }
 
-extern "C" int pvq_fp8_input_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes)
+extern "C" int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes)
 {
-    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_result(m, n)})) return rc;
-    if (!known(out_dtype) || !bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? fp8_input_grad_work(m, n, k, out_dtype, 1) : 0;
+    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
+    if (!bytes) return PVQ_E_INVALID_ARG;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n) + fp8_input_grad_work(m, n, k, 1) : 0;
     return PVQ_OK;
 }
 
@@ -122,26 +137,28 @@ extern "C" int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const
                                   int64_t k, void *dX, int out_dtype, int64_t lddx, void *work, size_t work_bytes, void *stream)
 {
     size_t wanted = 0;
-    if (const int rc = pvq_fp8_input_grad_work_bytes(m, n, k, out_dtype, &wanted)) return rc;
+    if (const int rc = pvq_fp8_input_grad_work_bytes(dY, lddy, m, n, k, &wanted)) return rc;
+    if (!known(out_dtype)) return PVQ_E_INVALID_ARG;
     if (m == 0 || k == 0) return PVQ_OK;
     fp8_grad_args a{};
     a.pairs = 1;
     a.dy[0] = {(const uint16_t *)dY, m, n, lddy};
     a.b[0] = {w_codes, w_exponents, n, k};
     a.out[0] = {dX, out_dtype, lddx};
-    a.work = (float *)work;
     if (const int rc = first_of({check_matrix(dX, out_dtype, k, lddx), n ? check_matrix(dY, PVQ_BF16, n, lddy) : PVQ_OK, check_blocks(a.b[0]),
                                  check_work(work, work_bytes, wanted)}))
         return rc;
-    if (n == 0) return status_of(fp8_launch_join(nullptr, 0, m, k, a.out[0], (hipStream_t)stream));
-    return status_of(fp8_launch_input_grad(a, (hipStream_t)stream));
+    const hipStream_t s = (hipStream_t)stream;
+    if (n == 0) return status_of(fp8_launch_join(nullptr, 0, m, k, a.out[0], s));
+    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n), s);
+    return status_of(e == hipSuccess ? fp8_launch_input_grad(a, s) : e);
 }
 
-extern "C" int pvq_fp8_weight_grad_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes)
+extern "C" int pvq_fp8_weight_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes)
 {
-    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_result(m, n)})) return rc;
-    if (!known(out_dtype) || !bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? fp8_weight_grad_work(m, n, k, out_dtype, 1) : 0;
+    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
+    if (!bytes) return PVQ_E_INVALID_ARG;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n) + fp8_weight_grad_work(m, n, k, 1) : 0;
     return PVQ_OK;
 }
 
@@ -149,31 +166,41 @@ extern "C" int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int6
                                    int64_t k, void *dW, int out_dtype, int64_t lddw, void *work, size_t work_bytes, void *stream)
 {
     size_t wanted = 0;
-    if (const int rc = pvq_fp8_weight_grad_work_bytes(m, n, k, out_dtype, &wanted)) return rc;
+    if (const int rc = pvq_fp8_weight_grad_work_bytes(dY, lddy, m, n, k, &wanted)) return rc;
+    if (!known(out_dtype)) return PVQ_E_INVALID_ARG;
     if (n == 0 || k == 0) return PVQ_OK;
     fp8_grad_args a{};
     a.pairs = 1;
     a.dy[0] = {(const uint16_t *)dY, m, n, lddy};
     a.b[0] = {x_codes, x_exponents, m, k};
     a.out[0] = {dW, out_dtype, lddw};
-    a.work = (float *)work;
     if (const int rc = first_of({check_matrix(dW, out_dtype, k, lddw), m ? check_matrix(dY, PVQ_BF16, n, lddy) : PVQ_OK, check_blocks(a.b[0]),
                                  check_work(work, work_bytes, wanted)}))
         return rc;
-    if (m == 0) return status_of(fp8_launch_join(nullptr, 0, n, k, a.out[0], (hipStream_t)stream));
-    return status_of(fp8_launch_weight_grad(a, (hipStream_t)stream));
+    const hipStream_t s = (hipStream_t)stream;
+    if (m == 0) return status_of(fp8_launch_join(nullptr, 0, n, k, a.out[0], s));
+    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n), s);
+    return status_of(e == hipSuccess ? fp8_launch_weight_grad(a, s) : e);
+}
+
+extern "C" int pvq_fp8_gated_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, int to_blocks, size_t *bytes)
+{
+    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
+    if (!known(out_dtype) || !bytes) return PVQ_E_INVALID_ARG;
+    *bytes = m && n && k && (to_blocks || !fp8_rows_pay(m)) ? std::max(fp8_gated_work(m, n, k, false), fp8_gated_work(m, n, k, true)) : 0;
+    return PVQ_OK;
 }
 
 extern "C" int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m, const uint8_t *gate_codes,
                              const uint8_t *gate_exponents, const uint8_t *up_codes, const uint8_t *up_exponents, int64_t n, int64_t k,
                              int activation, void *H, int out_dtype, int64_t ldh, uint8_t *h_codes, uint8_t *h_exponents, uint8_t *g_codes,
-                             uint8_t *g_exponents, uint8_t *u_codes, uint8_t *u_exponents, void *stream)
+                             uint8_t *g_exponents, uint8_t *u_codes, uint8_t *u_exponents, void *work, size_t work_bytes, void *stream)
 {
-    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
-    if (activation != PVQ_SILU && activation != PVQ_GELU) return PVQ_E_INVALID_ARG;
-    if (H && !known(out_dtype)) return PVQ_E_INVALID_ARG;
-    if (m == 0 || n == 0) return PVQ_OK;
     const bool keep = g_codes || g_exponents || u_codes || u_exponents, encoded = h_codes || h_exponents;
+    size_t wanted = 0;
+    if (const int rc = pvq_fp8_gated_work_bytes(m, n, k, out_dtype, keep || encoded, &wanted)) return rc;
+    if (activation != PVQ_SILU && activation != PVQ_GELU) return PVQ_E_INVALID_ARG;
+    if (m == 0 || n == 0) return PVQ_OK;
     if (!H && !encoded) return PVQ_E_INVALID_ARG;
     fp8_gated_args a{};
     a.x = {x_codes, x_exponents, m, k};
@@ -182,19 +209,20 @@ extern "C" int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents,
     a.act = activation;
     a.h = {H, out_dtype, ldh};
     a.hc = h_codes; a.he = h_exponents; a.gc = g_codes; a.ge = g_exponents; a.uc = u_codes; a.ue = u_exponents;
+    a.work = (float *)work;
     if (const int rc = first_of({H ? check_matrix(H, out_dtype, n, ldh) : PVQ_OK, check_blocks(a.x), check_blocks(a.gate), check_blocks(a.up),
                                  encoded ? check_blocks({h_codes, h_exponents, m, n}) : PVQ_OK, keep ? check_blocks({g_codes, g_exponents, m, n}) : PVQ_OK,
-                                 keep ? check_blocks({u_codes, u_exponents, m, n}) : PVQ_OK}))
+                                 keep ? check_blocks({u_codes, u_exponents, m, n}) : PVQ_OK, check_work(work, work_bytes, wanted)}))
         return rc;
     return status_of(fp8_rows_pay(m) && !keep && !encoded && k > 0 ? fp8_launch_gated_rows(a, (hipStream_t)stream) : fp8_launch_gated(a, (hipStream_t)stream));
 }
 
-extern "C" int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, size_t *bytes)
+extern "C" int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes)
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
-    if (!known(out_dtype) || !bytes) return PVQ_E_INVALID_ARG;
+    if (!bytes) return PVQ_E_INVALID_ARG;
     const size_t slopes = up16((size_t)m * slope_row(n) * 2);
-    const size_t sums = m && n && k ? std::max(fp8_input_grad_work(m, n, k, out_dtype, 2), fp8_weight_grad_work(m, n, k, out_dtype, 2)) : 0;
+    const size_t sums = m && n && k ? std::max(fp8_input_grad_work(m, n, k, 2), fp8_weight_grad_work(m, n, k, 2)) : 0;
     *bytes = 2 * slopes + sums;
     return PVQ_OK;
 }
@@ -206,7 +234,8 @@ extern "C" int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_
                                       void *dWu, int64_t lddw, int out_dtype, void *work, size_t work_bytes, void *stream)
 {
     size_t wanted = 0;
-    if (const int rc = pvq_fp8_gated_backward_work_bytes(m, n, k, out_dtype, &wanted)) return rc;
+    if (const int rc = pvq_fp8_gated_backward_work_bytes(m, n, k, &wanted)) return rc;
+    if (!known(out_dtype)) return PVQ_E_INVALID_ARG;
     if (activation != PVQ_SILU && activation != PVQ_GELU) return PVQ_E_INVALID_ARG;
     if (!dWg != !dWu || (!dX && !dWg)) return PVQ_E_INVALID_ARG;
     if (k == 0) return PVQ_OK;

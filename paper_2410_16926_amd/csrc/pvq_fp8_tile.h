@@ -72,7 +72,7 @@ __device__ inline void sums_are_there()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-__device__ inline f32x4 read_sums(const f32x4 &c)
+__device__ __forceinline__ f32x4 read_sums(const f32x4 &c)
 {
     f32x4 v;
 #pragma unroll
@@ -86,14 +86,14 @@ __device__ inline f32x4 read_sums(const f32x4 &c)
 
 // 8-bit instruction, 16 x 16 x 128, with byte AT of words of four exponents
 template <int AT>
-__device__ inline void multiply_accumulated(f32x4 &c, i32x8 a, uint32_t ea, i32x8 b, uint32_t eb)
+__device__ __forceinline__ void multiply_accumulated(f32x4 &c, i32x8 a, uint32_t ea, i32x8 b, uint32_t eb)
 {
     asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%5,0] op_sel_hi:[%6,%6,0]"
                  : "+a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(AT & 1), "n"(AT >> 1));
 }
 
 // bfloat16 instruction, 16 x 16 x 32
-__device__ inline void multiply_accumulated(f32x4 &c, bf16x8 a, bf16x8 b)
+__device__ __forceinline__ void multiply_accumulated(f32x4 &c, bf16x8 a, bf16x8 b)
 {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
@@ -101,7 +101,7 @@ __device__ inline void multiply_accumulated(f32x4 &c, bf16x8 a, bf16x8 b)
 // FM x FN fragments of 16 x 16 of a result to memory, from row0 and col0 on, rows and columns the result's.  A lane has four neighbouring columns of one
 // row: columns 4 (lane / 16 % 4) .. of a fragment, row lane % 16.  vec: what y's rows are aligned to, 8 values, 4 or 1.
 template <int FM, int FN, typename V>
-__device__ inline void store_fragments(const fp8_matrix &y, int vec, int64_t rows, int64_t cols, int64_t row0, int64_t col0, V value)
+__device__ __forceinline__ void store_fragments(const fp8_matrix &y, int vec, int64_t rows, int64_t cols, int64_t row0, int64_t col0, V value)
 {
     const int lane = threadIdx.x % kWave, r16 = lane % 16, quarter = lane / 16;
     if (vec == 8 && row0 + FM * 16 <= rows && col0 + FN * 16 <= cols) {

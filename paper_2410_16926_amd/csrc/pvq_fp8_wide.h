@@ -1,0 +1,221 @@
+// Sums of a tile of 256 x 256 on the bfloat16 matrix instruction, from 8-bit blocks that are decoded, exactly, on their way into LDS:
+//   out(i, j) = sum over r of A(i, r) B(r, j)
+// for products whose sums are to be those of 32 bits, and for the gradients.
+#pragma once
+
+#include "pvq_fp8_tile.h"
+
+namespace pvq_fp8_dev {
+
+constexpr int kWideTile = 256, kWideStep = 64, kWideLds = 4 * kWideTile * kWideStep * 2;
+
+enum wide_kind {
+    WIDE_PRODUCT,        // A and B in blocks along the sum: A(i, r) = a[i][r], B(r, j) = b[j][r]
+    WIDE_INPUT_GRAD,     // A(i, r) = dy[i][r], B(r, j) = b[r][j]; one or two terms
+    WIDE_WEIGHT_GRAD,    // A(i, r) = dy[r][i], B(r, j) = b[r][j]
+};
+
+struct wide_args {
+    fp8_bf16 dy[2];                  // of the terms, or of the outputs; rows aligned to 16 bytes
+    fp8_blocks a, b[2];              // b: of the terms or outputs; the gate's and the up weights
+    fp8_matrix out[2];
+    int64_t rows, cols, depth;       // of the output, and of the sum (one term's); GATED: cols are hidden units
+    int terms;                       // of the sum
+    int tiles_i, tiles_j;
+    int parts, steps_a_part;         // of a split sum, whose parts go to work
+    float *work;
+    int vec;                         // what the outputs' rows are aligned to: 8 values, 4 or 1
+};
+
+// Steps first .. last of the tile at i0, j0.  Four waves of 128 x 128, one to a SIMD, as for products on the 8-bit instruction
+// (pvq_fp8_product.hip): LDS is written 64 KB and read 128 KB for 64 of the sum, 1500 of the 2048 cycles of matrix instructions.  Both operands come
+// through registers, codes to be decoded once for the four waves, dY as it is.
+//
+// A step is 64 of the sum, two halves of 32.  While the first half's 64 instructions run, the second half's operands are read, which empties the
+// stage; behind the step's barrier, while the second half's run, the next step's first operands are read from the other stage, then what was fetched
+// a step ago is put into the empty one, and the step after that is fetched.
+//
+// GATED (WIDE_PRODUCT): the tile's 256 columns are 128 hidden units of the gate weights and the same of the up weights; a wave has both for its 64.
+template <int KIND, bool GATED>
+__device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int64_t i0, int64_t j0, int out_of, int first, int last, f32x4 (&acc)[8][8])
+{
+    constexpr int F = 8, kPlane = kWideTile * kWideStep * 2, kPieces = 8;       // LDS: A's two stages, B's two stages
+    constexpr bool A_ALONG = KIND != WIDE_WEIGHT_GRAD, B_ALONG = KIND == WIDE_PRODUCT, A_CODES = KIND == WIDE_PRODUCT;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int wi = wave / 2, wj = wave % 2, r16 = lane % 16, quarter = lane / 16;
+    const int steps_a_term = (int)((t.depth + kWideStep - 1) / kWideStep);
+
+    // Strides in bytes (the same for both terms or outputs).  A lane's piece is eight values of a row; an operand whose rows run along the sum has eight
+    // lanes to a row, one whose rows run across it 32, and piece p is 32 or 8 rows behind piece p - 1.
+    const uint32_t a_row = A_CODES ? (uint32_t)t.a.code_row() : (uint32_t)t.dy[0].ld * 2, b_row = (uint32_t)t.b[0].code_row();
+    const uint32_t ae_row = (uint32_t)t.a.exp_row(), be_row = (uint32_t)t.b[0].exp_row();
+    const uint32_t along_row = tid / 8, along_col = tid % 8 * 8, across_row = tid / 32, across_col = tid % 32 * 8;
+    const uint32_t a_at = (A_ALONG ? along_row * a_row + along_col * (A_CODES ? 1 : 2) : across_row * a_row + across_col * 2), a_next = (A_ALONG ? 32 : 8) * a_row;
+    const uint32_t b_at = B_ALONG ? along_row * b_row + along_col : across_row * b_row + across_col, b_next = (B_ALONG ? 32 : 8) * b_row;
+    const uint32_t be_at = B_ALONG ? along_row * be_row : across_row * be_row + across_col / kFp8Block, be_next = (B_ALONG ? 32 : 8) * be_row;
+
+    u32x4 ra[kPieces];               // (codes: the first two words, and the exponent)
+    u32x2 rb[kPieces];
+    uint32_t re[kPieces];
+    __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
+    // Buffers that start with the step's part of the tile and end with the matrix: what lies behind, and everything of a step behind the last,
+    // is zero.
+    int tail = 8;                    // of the lane's eight of a row of dY that runs along the sum, how many belong to it
+    auto aim = [&](int step) {
+        const int term = step >= steps_a_term ? 1 : 0;
+        const bool second = (term | out_of) != 0;
+        const int64_t r0 = (int64_t)(step - term * steps_a_term) * kWideStep;
+        auto buffer = [&](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at) {
+            const int64_t left = step <= last ? max(min((rows - 1) * row + row_bytes - at, (int64_t)0xFFFFFFFF), (int64_t)0) : 0;
+            return __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)base + at), 0, (uint32_t)left, 0x00020000);
+        };
+        const uint8_t *b_codes = second ? t.b[1].codes : t.b[0].codes, *b_exps = second ? t.b[1].exps : t.b[0].exps;
+        if constexpr (A_CODES) {
+            a_from = buffer(t.a.codes, a_row, t.rows, a_row, i0 * a_row + r0);
+            ae_from = buffer(t.a.exps, ae_row, t.rows, ae_row, i0 * ae_row + r0 / kFp8Block);
+        } else {
+            // (dY's last row to the end of its last 16 bytes: a load that is not whole would bring nothing)
+            const int64_t row_end = ((A_ALONG ? t.depth : t.rows) * 2 + 15) / 16 * 16;
+            const uint16_t *y = second ? t.dy[1].data : t.dy[0].data;
+            a_from = A_ALONG ? buffer(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2) : buffer(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2);
+            tail = (int)min(t.depth - r0 - along_col, (int64_t)8);
+        }
+        if constexpr (B_ALONG) {
+            b_from = buffer(t.b[0].codes, b_row, t.cols, b_row, j0 * b_row + r0);
+            be_from = buffer(t.b[0].exps, be_row, t.cols, be_row, j0 * be_row + r0 / kFp8Block);
+            u_from = GATED ? buffer(t.b[1].codes, b_row, t.cols, b_row, j0 * b_row + r0) : b_from;
+            ue_from = GATED ? buffer(t.b[1].exps, be_row, t.cols, be_row, j0 * be_row + r0 / kFp8Block) : be_from;
+        } else {
+            b_from = buffer(b_codes, b_row, t.depth, b_row, r0 * b_row + j0);
+            be_from = buffer(b_exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block);
+        }
+    };
+    auto fetch_a = [&](int p) {
+        if constexpr (A_CODES) {
+            const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(a_from, a_at, p * a_next, 0));
+            ra[p][0] = w[0]; ra[p][1] = w[1];
+            ra[p][2] = __builtin_amdgcn_raw_buffer_load_b8(ae_from, along_row * ae_row, p * 32 * ae_row, 0);
+        } else ra[p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_from, a_at, p * a_next, 0));
+    };
+    auto fetch_b = [&](int p) {
+        const bool up = GATED && p >= kPieces / 2;
+        const int in = up ? p - kPieces / 2 : p;
+        rb[p] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(up ? u_from : b_from, b_at, in * b_next, 0));
+        re[p] = __builtin_amdgcn_raw_buffer_load_b8(up ? ue_from : be_from, be_at, in * be_next, 0);
+    };
+
+    // Rows across the sum lie in LDS as in memory, [r][256 columns], in pieces of sixteen columns; the transposing read gives a lane four neighbouring r
+    // of one column.  Piece c of row r lies at place c ^ f(r), f = r % 4 + 4 (r / 8 % 2): the eight rows that 32 lanes read at once lie in different
+    // banks.  Rows along the sum: [row][64 r], chunk c (eight r) of row i at place c ^ (i / 2 % 8).
+    const uint32_t across_to = across_row * 512 + (((across_col / 16) ^ (across_row & 3)) << 5) + across_col % 16 * 2, across_odd = across_to ^ (4 << 5);
+    const uint32_t along_to = along_row * 128 + (((along_col / 8) ^ (along_row / 2 & 7)) << 4);
+    auto place = [&](bool along, int p) { return p * 4096 + (along ? along_to : p & 1 ? across_odd : across_to); };
+    // what lies behind the end of dY's row must not count, not even times zero
+    uint32_t keep[4];
+    auto keep_tail = [&]() {
+#pragma unroll
+        for (int e = 0; e < 4; e++) keep[e] = 2 * e + 1 < tail ? ~0u : 2 * e < tail ? 0xFFFFu : 0u;
+    };
+    // (stages by the offset of their planes, 0 or kPlane: one body for all steps, whose sums stay where they are)
+    auto put_a = [&](uint32_t stage, int p) {
+        uint8_t *to = lds + stage + place(A_ALONG, p);
+        if constexpr (A_CODES) *reinterpret_cast<bf16x8 *>(to) = bf16x8_of_codes(ra[p][0], ra[p][1], scale_of(ra[p][2]));
+        else {
+            u32x4 v = ra[p];
+            if constexpr (A_ALONG) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] &= keep[e];
+            }
+            *reinterpret_cast<u32x4 *>(to) = v;
+        }
+    };
+    auto put_b = [&](uint32_t stage, int p) {
+        *reinterpret_cast<bf16x8 *>(lds + stage + 2 * kPlane + place(B_ALONG, p)) = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
+    };
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const uint32_t sub = lane % 16, f = sub / 4 | (quarter & 1) << 2, row_at = (8 * quarter + sub / 4) * 512 + (sub % 4) * 8;
+    auto read_across = [&](uint32_t plane, int column, int h) {       // sixteen columns from 16 * column on
+        const uint8_t *from = lds + plane + h * 32 * 512 + (column / 8) * 256 + (((column % 8) ^ f) << 5) + row_at;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * 512));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto read_along = [&](uint32_t plane, int row, int h) {           // sixteen rows from `row` on
+        return *reinterpret_cast<const bf16x8 *>(lds + plane + (row + r16) * 128 + (((4 * h + quarter) ^ (r16 >> 1)) << 4));
+    };
+    auto read_a = [&](uint32_t stage, int i, int h) { return A_ALONG ? read_along(stage, wi * 128 + i * 16, h) : read_across(stage, wi * 8 + i, h); };
+    auto read_b = [&](uint32_t stage, int j, int h) {
+        return B_ALONG ? read_along(stage + 2 * kPlane, GATED ? (j / 4) * 128 + wj * 64 + (j % 4) * 16 : wj * 128 + j * 16, h) : read_across(stage + 2 * kPlane, wj * 8 + j, h);
+    };
+
+#pragma unroll
+    for (int i = 0; i < F; i++)
+#pragma unroll
+        for (int j = 0; j < F; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    bf16x8 a_op[2][F], b_op[2][F];
+
+    auto fetch_all = [&](int step) {
+        aim(step);
+#pragma unroll
+        for (int p = 0; p < kPieces; p++) { fetch_a(p); fetch_b(p); }
+    };
+    auto put_all = [&](uint32_t stage) {
+        keep_tail();
+#pragma unroll
+        for (int p = 0; p < kPieces; p++) { put_a(stage, p); put_b(stage, p); }
+    };
+    // the reads of a half's operands behind its predecessor's first 32 instructions
+    auto read_behind = [&](uint32_t stage, int slot, int h) {
+        if (slot % 2 == 0 && slot / 2 < F) b_op[h][slot / 2] = read_b(stage, slot / 2, h);
+        if (slot % 2 == 0 && slot / 2 >= F && slot / 2 < 2 * F) a_op[h][slot / 2 - F] = read_a(stage, slot / 2 - F, h);
+    };
+    if (first > last) { sums_are_there(); return; }
+    fetch_all(first);
+    put_all(0);
+    fetch_all(first + 1);
+    put_all(kPlane);
+    fetch_all(first + 2);
+    all_reads();
+    barrier();
+#pragma unroll
+    for (int j = 0; j < F; j++) b_op[0][j] = read_b(0, j, 0);
+#pragma unroll
+    for (int i = 0; i < F; i++) a_op[0][i] = read_a(0, i, 0);
+    uint32_t stage = 0;
+    for (int step = first; step <= last; step++, stage ^= kPlane) {
+#pragma unroll
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int j = 0; j < F; j++) {
+                multiply_accumulated(acc[i][j], b_op[0][j], a_op[0][i]);
+                read_behind(stage, i * F + j, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        all_reads();
+        barrier();
+        keep_tail();
+        aim(step + 3);
+#pragma unroll
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int j = 0; j < F; j++) {
+                multiply_accumulated(acc[i][j], b_op[1][j], a_op[1][i]);
+                const int slot = i * F + j;
+                read_behind(stage ^ kPlane, slot, 0);
+                if (slot >= 32 && slot % 4 == 1) { put_a(stage, (slot - 32) / 4); fetch_a((slot - 32) / 4); }
+                if (slot >= 32 && slot % 4 == 3) { put_b(stage, (slot - 32) / 4); fetch_b((slot - 32) / 4); }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+    all_reads();
+    sums_are_there();
+}
+
+// steps of the tile's part
+__device__ inline void wide_steps(const wide_args &t, int part, int &first, int &last)
+{
+    const int steps = (int)((t.depth + kWideStep - 1) / kWideStep) * t.terms;
+    first = part * t.steps_a_part;
+    last = min(first + t.steps_a_part, steps) - 1;
+}
+
+}  // namespace pvq_fp8_dev

@@ -388,7 +388,7 @@ PyObject *fp8_input_grad(PyObject *const *a)
     const c10::DeviceGuard guard(device);
     const floats dx = result_of(a[7], a[6], m, k, w.codes);
     size_t bytes = 0;
-    if (const int status = pvq_fp8_input_grad_work_bytes(m, n, k, dx.dtype, &bytes)) return PyLong_FromLong(status);
+    if (const int status = pvq_fp8_input_grad_work_bytes(dy.p(), dy.ld, m, n, k, &bytes)) return PyLong_FromLong(status);
     const scratch work(bytes, w.codes);
     void *stream = current_stream();
     int status;
@@ -409,7 +409,7 @@ PyObject *fp8_weight_grad(PyObject *const *a)
     const c10::DeviceGuard guard(device);
     const floats dw = result_of(a[7], a[6], n, k, x.codes);
     size_t bytes = 0;
-    if (const int status = pvq_fp8_weight_grad_work_bytes(m, n, k, dw.dtype, &bytes)) return PyLong_FromLong(status);
+    if (const int status = pvq_fp8_weight_grad_work_bytes(dy.p(), dy.ld, m, n, k, &bytes)) return PyLong_FromLong(status);
     const scratch work(bytes, x.codes);
     void *stream = current_stream();
     int status;
@@ -435,13 +435,16 @@ PyObject *fp8_gated(PyObject *const *a)
     if (encoded) hb = new_blocks(m, n, x.codes);
     else h = result_of(a[11], a[10], m, n, x.codes);
     if (keep) { g = new_blocks(m, n, x.codes); u = new_blocks(m, n, x.codes); }
+    size_t bytes = 0;
+    if (const int status = pvq_fp8_gated_work_bytes(m, n, k, h.dtype, encoded || keep, &bytes)) return PyLong_FromLong(status);
+    const scratch work(bytes, x.codes);
     void *stream = current_stream();
     int status;
     {
         without_lock unlocked;
         status = pvq_fp8_gated(x.c(), x.e(), m, gate.c(), gate.e(), up.c(), up.e(), n, k, act, encoded ? nullptr : h.p(), h.dtype, h.ld,
                                encoded ? hb.c() : nullptr, encoded ? hb.e() : nullptr, keep ? g.c() : nullptr, keep ? g.e() : nullptr,
-                               keep ? u.c() : nullptr, keep ? u.e() : nullptr, stream);
+                               keep ? u.c() : nullptr, keep ? u.e() : nullptr, work.p(), bytes, stream);
     }
     if (status) return PyLong_FromLong(status);
     PyObject *first = encoded ? wrap(hb) : THPVariable_Wrap(h.t);
@@ -470,7 +473,7 @@ PyObject *fp8_gated_backward(PyObject *const *a)
     if (want_x) dx = new_tensor({m, k}, type, x.codes);
     if (want_w) { dwg = new_tensor({n, k}, type, x.codes); dwu = new_tensor({n, k}, type, x.codes); }
     size_t bytes = 0;
-    if (const int status = pvq_fp8_gated_backward_work_bytes(m, n, k, dtype, &bytes)) return PyLong_FromLong(status);
+    if (const int status = pvq_fp8_gated_backward_work_bytes(m, n, k, &bytes)) return PyLong_FromLong(status);
     const scratch work(bytes, x.codes);
     void *stream = current_stream();
     int status;

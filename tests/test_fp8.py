@@ -73,8 +73,9 @@ def test_encode_and_decode_refuse():
 def test_products_refuse():
     L = pvq.lib()
 
+    # (a workspace that is large enough, for the shapes that want one)
     def product(m=2, n=3, k=5, a=(A16, A16), b=(A16, A16), y=A16, t=F32, ld=3):
-        return L.pvq_fp8_product(*a, m, *b, n, k, y, t, ld, None, 0, None)
+        return L.pvq_fp8_product(*a, m, *b, n, k, y, t, ld, A16, 1 << 40, None)
     assert product(m=0) == 0 and product(n=0) == 0
     assert product(y=None) == product(ld=2) == product(t=7) == product(m=-1) == product(n=-1) == product(k=-1) == INVALID
     assert product(a=(None, A16)) == product(b=(A16, None)) == INVALID
@@ -82,13 +83,13 @@ def test_products_refuse():
     assert product(k=(1 << 22) + 1) == UNSUPPORTED
 
     def dx(m=2, n=3, k=5, dy=A16, lddy=3, w=(A16, A16), out=A16, t=F32, ld=5):
-        return L.pvq_fp8_input_grad(dy, lddy, m, *w, n, k, out, t, ld, None, 0, None)
+        return L.pvq_fp8_input_grad(dy, lddy, m, *w, n, k, out, t, ld, A16, 1 << 40, None)
     assert dx(m=0) == 0 and dx(k=0) == 0
     assert dx(dy=None) == dx(lddy=2) == dx(ld=4) == dx(out=None) == dx(w=(A16, None)) == dx(t=-1) == dx(n=-1) == INVALID
     assert dx(dy=ODD) == dx(w=(A16 + 8, A16)) == dx(out=A16 + 2) == ALIGNMENT
 
     def dw(m=2, n=3, k=5, dy=A16, lddy=3, x=(A16, A16), out=A16, t=F32, ld=5):
-        return L.pvq_fp8_weight_grad(dy, lddy, m, n, *x, k, out, t, ld, None, 0, None)
+        return L.pvq_fp8_weight_grad(dy, lddy, m, n, *x, k, out, t, ld, A16, 1 << 40, None)
     assert dw(n=0) == 0 and dw(k=0) == 0
     assert dw(dy=None) == dw(lddy=2) == dw(ld=4) == dw(out=None) == dw(x=(None, A16)) == dw(t=9) == INVALID
     assert dw(dy=ODD) == dw(x=(A16, A16 + 2)) == dw(out=A16 + 2) == ALIGNMENT
@@ -98,7 +99,7 @@ def test_the_gated_block_refuses():
     L = pvq.lib()
 
     def gated(m=2, n=3, k=5, act=0, h=A16, t=BF16, ld=3, hb=(None, None), kept=(None,) * 4, x=(A16, A16), g=(A16, A16), u=(A16, A16)):
-        return L.pvq_fp8_gated(*x, m, *g, *u, n, k, act, h, t, ld, *hb, *kept, None)
+        return L.pvq_fp8_gated(*x, m, *g, *u, n, k, act, h, t, ld, *hb, *kept, A16, 1 << 40, None)
     assert gated(m=0) == 0 and gated(n=0) == 0
     assert gated(act=2) == gated(t=5) == gated(ld=2) == gated(h=None) == INVALID
     assert gated(h=None, hb=(A16, None)) == gated(kept=(A16, A16, A16, None)) == gated(kept=(A16, A16, None, None)) == INVALID
@@ -111,14 +112,33 @@ def test_the_gated_block_refuses():
     assert backward(act=-1) == backward(dh=None) == backward(lddh=2) == backward(ldx=4) == backward(ldw=4) == backward(t=3) == INVALID
     assert backward(dx=None, dw=(None, None)) == backward(dw=(A16, None)) == backward(work=None) == INVALID
     need = C.c_size_t()
-    assert L.pvq_fp8_gated_backward_work_bytes(2, 3, 5, BF16, C.byref(need)) == 0 and need.value > 0
+    assert L.pvq_fp8_gated_backward_work_bytes(2, 3, 5, C.byref(need)) == 0 and need.value > 0
     assert backward(size=need.value - 1) == INVALID
     for i in range(10):
         assert backward(b=tuple(None if j == i else A16 for j in range(10))) == INVALID
     assert backward(work=A16 + 8) == backward(dh=ODD) == ALIGNMENT
-    for name in ("product", "input_grad", "weight_grad", "gated_backward"):
-        f = getattr(L, f"pvq_fp8_{name}_work_bytes")
-        assert f(2, 3, 5, BF16, None) == f(2, 3, 5, 4, C.byref(need)) == f(-1, 3, 5, F32, C.byref(need)) == INVALID
+    # workspaces: sizes, and calls whose workspace is missing, too small or not aligned
+    f = L.pvq_fp8_product_work_bytes
+    assert f(2, 3, 5, BF16, None) == f(2, 3, 5, 4, C.byref(need)) == f(-1, 3, 5, F32, C.byref(need)) == INVALID
+    f = L.pvq_fp8_gated_work_bytes
+    assert f(2, 3, 5, BF16, 0, None) == f(2, 3, 5, 4, 0, C.byref(need)) == f(2, 3, -5, F32, 0, C.byref(need)) == INVALID
+    assert f(1, 28672, 8192, BF16, 0, C.byref(need)) == 0 and need.value == 0
+    assert L.pvq_fp8_gated_backward_work_bytes(2, 3, 5, None) == L.pvq_fp8_gated_backward_work_bytes(2, -3, 5, C.byref(need)) == INVALID
+    for f in (L.pvq_fp8_input_grad_work_bytes, L.pvq_fp8_weight_grad_work_bytes):
+        assert f(A16, 8, 2, 8, 5, None) == f(A16, 8, 2, -8, 5, C.byref(need)) == INVALID
+        assert f(A16, 1 << 23, 1, (1 << 22) + 1, 5, C.byref(need)) == UNSUPPORTED
+        assert f(A16, 8, 2, 8, 5, C.byref(need)) == 0 and need.value == 0
+        assert f(A16 + 2, 8, 2, 8, 5, C.byref(need)) == 0 and need.value >= 2 * 8 * 2        # rows that do not start at 16 bytes
+        assert f(A16, 9, 2, 8, 5, C.byref(need)) == 0 and need.value >= 2 * 8 * 2
+    size = need.value
+    for work, n, want in ((None, 1 << 40, INVALID), (A16, size - 1, INVALID), (A16 + 8, 1 << 40, ALIGNMENT)):
+        assert L.pvq_fp8_input_grad(A16, 9, 2, A16, A16, 8, 5, A16, F32, 5, work, n, None) == want
+        assert L.pvq_fp8_weight_grad(A16, 9, 2, 8, A16, A16, 5, A16, F32, 5, work, n, None) == want
+    assert L.pvq_fp8_product_work_bytes(100, 100, 100000, BF16, C.byref(need)) == 0 and need.value > 0     # few tiles, a long sum: split
+    assert L.pvq_fp8_product(A16, A16, 100, A16, A16, 100, 100000, A16, BF16, 100, None, 0, None) == INVALID
+    assert L.pvq_fp8_product(A16, A16, 100, A16, A16, 100, 100000, A16, BF16, 100, A16, need.value - 1, None) == INVALID
+    assert L.pvq_fp8_gated_work_bytes(100, 100, 100000, BF16, 0, C.byref(need)) == 0 and need.value > 0
+    assert L.pvq_fp8_gated(A16, A16, 100, A16, A16, A16, A16, 100, 100000, 0, A16, BF16, 100, *[None] * 6, A16, need.value - 1, None) == INVALID
 
 
 def test_the_binding_refuses_what_is_not_on_a_gpu():
