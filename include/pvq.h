@@ -364,7 +364,7 @@ int pvq_fp8_product(const uint8_t *a_codes, const uint8_t *a_exponents, int64_t 
  *   pvq_fp8_weight_grad   dW = dY^T X  [n][lddw] of out_dtype
  * On the bfloat16 matrix instructions, the blocks decoded exactly, sums in float32 and one rounding to out_dtype.
  * work as for pvq_fp8_product; its size depends on dY and lddy by their alignment alone (rows that do not start at 16 bytes are copied
- * there first).
+ * there first, for dX also those whose n is no multiple of 64).
  */
 int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const uint8_t *w_codes, const uint8_t *w_exponents, int64_t n,

@@ -16,7 +16,7 @@ enum wide_kind {
 };
 
 struct wide_args {
-    fp8_bf16 dy[2];                  // of the terms, or of the outputs; rows aligned to 16 bytes
+    fp8_bf16 dy[2];                  // of the terms, or of the outputs; rows aligned to 16 bytes, for input gradients whole 64s or zeros behind their last value
     fp8_blocks a, b[2];              // b: of the terms or outputs; the gate's and the up weights
     fp8_matrix out[2];
     int64_t rows, cols, depth;       // of the output, and of the sum (one term's); GATED: cols are hidden units
@@ -33,7 +33,9 @@ struct wide_args {
 //
 // A step is 64 of the sum, two halves of 32.  While the first half's 64 instructions run, the second half's operands are read, which empties the
 // stage; behind the step's barrier, while the second half's run, the next step's first operands are read from the other stage, then what was fetched
-// a step ago is put into the empty one, and the step after that is fetched.
+// a step ago is put into the empty one.  One operand's codes are decoded in the first half, the other's in the second, and either is fetched again as
+// soon as its registers are free: a wave alone on its SIMD has about three instructions to issue beside each matrix instruction, and what does not fit
+// holds the next one up (all of it in the second half: 478 us for dX of 2048 x 2 x 14336 x 4096).
 //
 // GATED (WIDE_PRODUCT): the tile's 256 columns are 128 hidden units of the gate weights and the same of the up weights; a wave has both for its 64.
 template <int KIND, bool GATED>
@@ -53,48 +55,68 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     const uint32_t a_at = (A_ALONG ? along_row * a_row + along_col * (A_CODES ? 1 : 2) : across_row * a_row + across_col * 2), a_next = (A_ALONG ? 32 : 8) * a_row;
     const uint32_t b_at = B_ALONG ? along_row * b_row + along_col : across_row * b_row + across_col, b_next = (B_ALONG ? 32 : 8) * b_row;
     const uint32_t be_at = B_ALONG ? along_row * be_row : across_row * be_row + across_col / kFp8Block, be_next = (B_ALONG ? 32 : 8) * be_row;
+    const uint32_t ae_at = along_row * ae_row, ae_next = 32 * ae_row;
 
     u32x4 ra[kPieces];               // (codes: the first two words, and the exponent)
     u32x2 rb[kPieces];
     uint32_t re[kPieces];
-    __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
-    // Buffers that start with the step's part of the tile and end with the matrix: what lies behind, and everything of a step behind the last,
-    // is zero.
-    int tail = 8;                    // of the lane's eight of a row of dY that runs along the sum, how many belong to it
-    auto aim = [&](int step) {
+    bf16x8 decoded[kPieces];         // A's codes, or else B's, for the next half
+    // Where a step's part of an operand's tile starts, and how much of the matrix is left there: what lies behind, and everything of a step
+    // behind the last, is zero.
+    struct source {
+        const uint8_t *p;
+        int64_t left, step;          // step: bytes to the next step
+    };
+    auto source_of = [](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at, int64_t step) {
+        return source{(const uint8_t *)base + at, (rows - 1) * row + row_bytes - at, step};
+    };
+    source a_src, b_src, u_src, ae_src, be_src, ue_src;
+    auto start = [&](int step) {                  // at the first step, and where the second term begins
         const int term = step >= steps_a_term ? 1 : 0;
         const bool second = (term | out_of) != 0;
         const int64_t r0 = (int64_t)(step - term * steps_a_term) * kWideStep;
-        auto buffer = [&](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at) {
-            const int64_t left = step <= last ? max(min((rows - 1) * row + row_bytes - at, (int64_t)0xFFFFFFFF), (int64_t)0) : 0;
-            return __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)base + at), 0, (uint32_t)left, 0x00020000);
-        };
-        const uint8_t *b_codes = second ? t.b[1].codes : t.b[0].codes, *b_exps = second ? t.b[1].exps : t.b[0].exps;
+        const fp8_blocks b = {second ? t.b[1].codes : t.b[0].codes, second ? t.b[1].exps : t.b[0].exps, 0, 0};
         if constexpr (A_CODES) {
-            a_from = buffer(t.a.codes, a_row, t.rows, a_row, i0 * a_row + r0);
-            ae_from = buffer(t.a.exps, ae_row, t.rows, ae_row, i0 * ae_row + r0 / kFp8Block);
+            a_src = source_of(t.a.codes, a_row, t.rows, a_row, i0 * a_row + r0, kWideStep);
+            ae_src = source_of(t.a.exps, ae_row, t.rows, ae_row, i0 * ae_row, 0);
         } else {
             // (dY's last row to the end of its last 16 bytes: a load that is not whole would bring nothing)
-            const int64_t row_end = ((A_ALONG ? t.depth : t.rows) * 2 + 15) / 16 * 16;
+            const int64_t row_end = ((A_ALONG ? (t.depth + kWideStep - 1) / kWideStep * kWideStep : t.rows) * 2 + 15) / 16 * 16;
             const uint16_t *y = second ? t.dy[1].data : t.dy[0].data;
-            a_from = A_ALONG ? buffer(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2) : buffer(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2);
-            tail = (int)min(t.depth - r0 - along_col, (int64_t)8);
+            a_src = A_ALONG ? source_of(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2, kWideStep * 2) : source_of(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2, (int64_t)kWideStep * a_row);
         }
         if constexpr (B_ALONG) {
-            b_from = buffer(t.b[0].codes, b_row, t.cols, b_row, j0 * b_row + r0);
-            be_from = buffer(t.b[0].exps, be_row, t.cols, be_row, j0 * be_row + r0 / kFp8Block);
-            u_from = GATED ? buffer(t.b[1].codes, b_row, t.cols, b_row, j0 * b_row + r0) : b_from;
-            ue_from = GATED ? buffer(t.b[1].exps, be_row, t.cols, be_row, j0 * be_row + r0 / kFp8Block) : be_from;
+            b_src = source_of(t.b[0].codes, b_row, t.cols, b_row, j0 * b_row + r0, kWideStep);
+            be_src = source_of(t.b[0].exps, be_row, t.cols, be_row, j0 * be_row, 0);
+            u_src = GATED ? source_of(t.b[1].codes, b_row, t.cols, b_row, j0 * b_row + r0, kWideStep) : b_src;
+            ue_src = GATED ? source_of(t.b[1].exps, be_row, t.cols, be_row, j0 * be_row, 0) : be_src;
         } else {
-            b_from = buffer(b_codes, b_row, t.depth, b_row, r0 * b_row + j0);
-            be_from = buffer(b_exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block);
+            b_src = source_of(b.codes, b_row, t.depth, b_row, r0 * b_row + j0, (int64_t)kWideStep * b_row);
+            be_src = source_of(b.exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block, (int64_t)kWideStep * be_row);
         }
+    };
+    __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
+    auto take = [&](source &s, int step, int64_t more = 0) {       // the buffer of a step, and on to the next
+        const int64_t left = step <= last ? min(s.left - more, (int64_t)0xFFFFFFFF) : 0;
+        const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)(s.p + more), 0, (uint32_t)(left < 0 ? 0 : left), 0x00020000);
+        s.p += s.step;
+        s.left -= s.step;
+        return r;
+    };
+    auto aim = [&](int step) {
+        if (KIND == WIDE_INPUT_GRAD && step == steps_a_term) start(step);
+        // (rows along the sum: an exponent is that of two steps)
+        a_from = take(a_src, step);
+        if constexpr (A_CODES) ae_from = take(ae_src, step, step / 2);
+        b_from = take(b_src, step);
+        be_from = take(be_src, step, B_ALONG ? step / 2 : 0);
+        if constexpr (GATED) { u_from = take(u_src, step); ue_from = take(ue_src, step, step / 2); }
     };
     auto fetch_a = [&](int p) {
         if constexpr (A_CODES) {
             const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(a_from, a_at, p * a_next, 0));
             ra[p][0] = w[0]; ra[p][1] = w[1];
-            ra[p][2] = __builtin_amdgcn_raw_buffer_load_b8(ae_from, along_row * ae_row, p * 32 * ae_row, 0);
+            ra[p][2] = __builtin_amdgcn_raw_buffer_load_b8(ae_from, ae_at, p * ae_next, 0);
         } else ra[p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_from, a_at, p * a_next, 0));
     };
     auto fetch_b = [&](int p) {
@@ -110,27 +132,20 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     const uint32_t across_to = across_row * 512 + (((across_col / 16) ^ (across_row & 3)) << 5) + across_col % 16 * 2, across_odd = across_to ^ (4 << 5);
     const uint32_t along_to = along_row * 128 + (((along_col / 8) ^ (along_row / 2 & 7)) << 4);
     auto place = [&](bool along, int p) { return p * 4096 + (along ? along_to : p & 1 ? across_odd : across_to); };
-    // what lies behind the end of dY's row must not count, not even times zero
-    uint32_t keep[4];
-    auto keep_tail = [&]() {
-#pragma unroll
-        for (int e = 0; e < 4; e++) keep[e] = 2 * e + 1 < tail ? ~0u : 2 * e < tail ? 0xFFFFu : 0u;
-    };
     // (stages by the offset of their planes, 0 or kPlane: one body for all steps, whose sums stay where they are)
+    auto decode = [&](int p) {
+        if constexpr (A_CODES) decoded[p] = bf16x8_of_codes(ra[p][0], ra[p][1], scale_of(ra[p][2]));
+        else decoded[p] = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
+    };
     auto put_a = [&](uint32_t stage, int p) {
         uint8_t *to = lds + stage + place(A_ALONG, p);
-        if constexpr (A_CODES) *reinterpret_cast<bf16x8 *>(to) = bf16x8_of_codes(ra[p][0], ra[p][1], scale_of(ra[p][2]));
-        else {
-            u32x4 v = ra[p];
-            if constexpr (A_ALONG) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) v[e] &= keep[e];
-            }
-            *reinterpret_cast<u32x4 *>(to) = v;
-        }
+        if constexpr (A_CODES) *reinterpret_cast<bf16x8 *>(to) = decoded[p];
+        else *reinterpret_cast<u32x4 *>(to) = ra[p];
     };
     auto put_b = [&](uint32_t stage, int p) {
-        *reinterpret_cast<bf16x8 *>(lds + stage + 2 * kPlane + place(B_ALONG, p)) = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
+        bf16x8 *to = reinterpret_cast<bf16x8 *>(lds + stage + 2 * kPlane + place(B_ALONG, p));
+        if constexpr (A_CODES) *to = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
+        else *to = decoded[p];
     };
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const uint32_t sub = lane % 16, f = sub / 4 | (quarter & 1) << 2, row_at = (8 * quarter + sub / 4) * 512 + (sub % 4) * 8;
@@ -159,9 +174,8 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
         for (int p = 0; p < kPieces; p++) { fetch_a(p); fetch_b(p); }
     };
     auto put_all = [&](uint32_t stage) {
-        keep_tail();
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) { put_a(stage, p); put_b(stage, p); }
+        for (int p = 0; p < kPieces; p++) { decode(p); put_a(stage, p); put_b(stage, p); }
     };
     // the reads of a half's operands behind its predecessor's first 32 instructions
     auto read_behind = [&](uint32_t stage, int slot, int h) {
@@ -169,6 +183,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
         if (slot % 2 == 0 && slot / 2 >= F && slot / 2 < 2 * F) a_op[h][slot / 2 - F] = read_a(stage, slot / 2 - F, h);
     };
     if (first > last) { sums_are_there(); return; }
+    start(first);
     fetch_all(first);
     put_all(0);
     fetch_all(first + 1);
@@ -182,18 +197,23 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     for (int i = 0; i < F; i++) a_op[0][i] = read_a(0, i, 0);
     uint32_t stage = 0;
     for (int step = first; step <= last; step++, stage ^= kPlane) {
+        aim(step + 3);
 #pragma unroll
         for (int i = 0; i < F; i++)
 #pragma unroll
             for (int j = 0; j < F; j++) {
                 multiply_accumulated(acc[i][j], b_op[0][j], a_op[0][i]);
-                read_behind(stage, i * F + j, 1);
+                const int slot = i * F + j;
+                read_behind(stage, slot, 1);
+                if (slot >= 32 && slot % 4 == 1) {
+                    decode((slot - 32) / 4);
+                    if (A_CODES) fetch_a((slot - 32) / 4);
+                    else fetch_b((slot - 32) / 4);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         all_reads();
         barrier();
-        keep_tail();
-        aim(step + 3);
 #pragma unroll
         for (int i = 0; i < F; i++)
 #pragma unroll
@@ -201,8 +221,14 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
                 multiply_accumulated(acc[i][j], b_op[1][j], a_op[1][i]);
                 const int slot = i * F + j;
                 read_behind(stage ^ kPlane, slot, 0);
-                if (slot >= 32 && slot % 4 == 1) { put_a(stage, (slot - 32) / 4); fetch_a((slot - 32) / 4); }
-                if (slot >= 32 && slot % 4 == 3) { put_b(stage, (slot - 32) / 4); fetch_b((slot - 32) / 4); }
+                if (slot >= 32 && slot % 4 == 1) {
+                    put_a(stage, (slot - 32) / 4);
+                    if (!A_CODES) fetch_a((slot - 32) / 4);
+                }
+                if (slot >= 32 && slot % 4 == 3) {
+                    put_b(stage, (slot - 32) / 4);
+                    if (A_CODES) fetch_b((slot - 32) / 4);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
     }
