@@ -71,53 +71,63 @@ __device__ inline bf16x8 bf16x8_of_codes(uint32_t lo, uint32_t hi, float scale)
     return __builtin_bit_cast(bf16x8, w);
 }
 
-// Four neighbouring values of a row to out[row][col ..], of which `count` lie inside.  VEC: `out` and its rows are aligned
-// to four values.
-template <bool VEC>
-__device__ inline void store4(const fp8_matrix &y, int64_t row, int64_t col, int64_t count, f32x4 v)
+// Vectors at any element's address: loads and stores of global memory need no more alignment than that.
+template <typename V, int ALIGNMENT>
+struct __attribute__((packed, aligned(ALIGNMENT))) unaligned { V v; };
+template <typename V>
+__device__ inline void store_vector(float *p, V v) { reinterpret_cast<unaligned<V, 4> *>(p)->v = v; }
+template <typename V>
+__device__ inline void store_vector(uint16_t *p, V v) { reinterpret_cast<unaligned<V, 2> *>(p)->v = v; }
+
+// Neighbouring values of a row, four or eight, to out[row][col ..], of which `count` lie inside.
+template <int N>
+__device__ inline void store_values(const fp8_matrix &y, int64_t row, int64_t col, int64_t count, const float (&v)[N])
 {
     const int64_t at = row * y.ld + col;
     if (y.dtype == PVQ_F32) {
         float *p = reinterpret_cast<float *>(y.data) + at;
-        if (VEC && count >= 4) { *reinterpret_cast<f32x4 *>(p) = v; return; }
+        if (count >= N) {
 #pragma unroll
-        for (int i = 0; i < 4; i++) if (i < count) p[i] = v[i];
+            for (int i = 0; i < N; i += 4) store_vector(p + i, f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]});
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; i++) if (i < count) p[i] = v[i];
         return;
     }
-    const u32x2 w = y.dtype == PVQ_BF16 ? u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])} : u32x2{f16_pair(v[0], v[1]), f16_pair(v[2], v[3])};
-    uint16_t *p = reinterpret_cast<uint16_t *>(y.data) + at;
-    if (VEC && count >= 4) { *reinterpret_cast<u32x2 *>(p) = w; return; }
+    typedef __attribute__((ext_vector_type(N / 2))) uint32_t words;
+    words w;
 #pragma unroll
-    for (int i = 0; i < 4; i++) if (i < count) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    for (int i = 0; i < N / 2; i++) w[i] = y.dtype == PVQ_BF16 ? bf16_pair(v[2 * i], v[2 * i + 1]) : f16_pair(v[2 * i], v[2 * i + 1]);
+    uint16_t *p = reinterpret_cast<uint16_t *>(y.data) + at;
+    if (count >= N) { store_vector(p, w); return; }
+#pragma unroll
+    for (int i = 0; i < N; i++) if (i < count) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
 }
 
-// The same of two fragments side by side (columns col .. and col + 16 .., a lane's four at 4 quarter of each): lanes of quarters 2 p and
-// 2 p + 1 exchange halves, so that each holds eight neighbouring columns, of the left fragment or the right one.  A row's store is
-// 64 bytes in a row in place of 32.  Only for what lies inside, in rows aligned to eight values; `col` is that of the left fragment.
-__device__ inline void store_pair(const fp8_matrix &y, int64_t row, int64_t col, int quarter, f32x4 left, f32x4 right)
+// the largest of a block's sixteen lanes, in all of them (rotations inside a row of sixteen)
+__device__ inline uint32_t block_max(uint32_t v)
 {
-    const int64_t at = row * y.ld + col + 16 * (quarter & 1) + 8 * (quarter >> 1);
-    if (y.dtype == PVQ_F32) {
-        u32x4 lo, hi;
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, false));
+}
+
+// the exponent of a block of which each of sixteen lanes has eight values
+__device__ inline uint32_t block_exponent(const float (&v)[8])
+{
+    uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(left[i]), __float_as_uint(right[i]), false, false);
-            lo[i] = r[0]; hi[i] = r[1];
-        }
-        u32x4 *p = reinterpret_cast<u32x4 *>(reinterpret_cast<float *>(y.data) + at);
-        p[0] = lo; p[1] = hi;
-        return;
-    }
-    const bool b = y.dtype == PVQ_BF16;
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const uint32_t l = b ? bf16_pair(left[2 * i], left[2 * i + 1]) : f16_pair(left[2 * i], left[2 * i + 1]);
-        const uint32_t r = b ? bf16_pair(right[2 * i], right[2 * i + 1]) : f16_pair(right[2 * i], right[2 * i + 1]);
-        const auto s = __builtin_amdgcn_permlane16_swap(l, r, false, false);
-        w[i] = s[0]; w[2 + i] = s[1];
-    }
-    *reinterpret_cast<u32x4 *>(reinterpret_cast<uint16_t *>(y.data) + at) = w;
+    for (int i = 0; i < 8; i++) top = max(top, finite_bits(v[i]));
+    return exponent_of(block_max(top));
+}
+
+// a lane's eight codes of a block
+__device__ inline void store_codes8(uint8_t *to, uint32_t e, const float (&v)[8])
+{
+    const float inverse = scale_of(254 - e);
+    *reinterpret_cast<u32x2 *>(to) = u32x2{codes4(v[0], v[1], v[2], v[3], inverse), codes4(v[4], v[5], v[6], v[7], inverse)};
 }
 
 // Activations.  sigma(x) = 1 / (1 + exp(-x)) by the hardware's 2^x and reciprocal, each off by about one place; exp(-x) may be
@@ -131,18 +141,20 @@ __device__ inline float gelu_argument(float g)
     return 1.5957691216057308f * (c + 0.044715f * c * c * c);       // 2 w
 }
 
-__device__ inline float act_value(int act, float g)
+template <int ACT>
+__device__ inline float act_value(float g)
 {
-    const float x = act == PVQ_SILU ? g : gelu_argument(g);
+    const float x = ACT == PVQ_SILU ? g : gelu_argument(g);
     return g * __builtin_amdgcn_rcpf(1.0f + exp_minus(x));
 }
 
 // act(g) and its derivative sigma + g sigma (1 - sigma) dx/dg.  1 - sigma is formed as sigma exp(-x), of full accuracy for
 // large x too; where exp(-x) is infinite sigma is 0 and so is the product.
-__device__ inline void act_slope(int act, float g, float &value, float &slope)
+template <int ACT>
+__device__ inline void act_slope(float g, float &value, float &slope)
 {
     float x = g, dx = 1.0f;
-    if (act != PVQ_SILU) {
+    if constexpr (ACT != PVQ_SILU) {
         const float c = fminf(fmaxf(g, -16.0f), 16.0f);
         x = gelu_argument(g);
         dx = 1.5957691216057308f * (1.0f + 3.0f * 0.044715f * c * c);
@@ -151,6 +163,42 @@ __device__ inline void act_slope(int act, float g, float &value, float &slope)
     value = g * s;
     const float rest = s > 0.0f ? s * e : 1.0f;                      // 1 - s
     slope = s + value * rest * dx;
+}
+
+// What the gated block stores, of eight neighbouring hidden units: H in floats and in blocks, G and U in blocks.
+struct gated_out {
+    fp8_matrix h;                // (data null: in blocks alone)
+    int act;
+    uint8_t *hc, *he, *gc, *ge, *uc, *ue;      // (null: not wanted)
+};
+
+// Sixteen lanes have the units of block `block` of a row, from col on eight each; all of them come here.  Units from n on are zeros in the codes.
+template <int ACT>
+__device__ inline void store_gated8(const gated_out &t, int64_t row, int64_t n, int64_t block, int64_t col, bool row_there, float (&g)[8], float (&u)[8])
+{
+    const int64_t count = n - col, code_row = (n + kFp8Block - 1) / kFp8Block * kFp8Block, exp_row = (code_row / kFp8Block + 3) / 4 * 4;
+    float h[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if (i >= count) g[i] = u[i] = 0.0f;
+        h[i] = act_value<ACT>(g[i]) * u[i];
+    }
+    if (t.h.data && row_there && count > 0) store_values(t.h, row, col, count, h);
+    auto to_blocks = [&](uint8_t *codes, uint8_t *exps, const float (&v)[8]) {
+        if (!codes) return;
+        const uint32_t e = block_exponent(v);
+        if (!row_there || block * kFp8Block >= n) return;
+        store_codes8(codes + row * code_row + col, e, v);
+        if (threadIdx.x % 16 == 0) {
+            uint8_t *p = exps + row * exp_row;
+            p[block] = (uint8_t)e;
+            if ((block + 1) * kFp8Block >= n)
+                for (int64_t b = block + 1; b < exp_row; b++) p[b] = 0;
+        }
+    };
+    to_blocks(t.gc, t.ge, g);
+    to_blocks(t.uc, t.ue, u);
+    to_blocks(t.hc, t.he, h);
 }
 
 // The workgroup's number such that those on one chiplet (the hardware deals them out in turn over 8) are neighbours, for any

@@ -9,7 +9,6 @@ template <int KIND>
 __global__ __launch_bounds__(256) void grad_kernel(wide_args t)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     int ti, tj, first, last;
     tile_of(t.tiles_i, t.tiles_j, chiplet_order(blockIdx.x, gridDim.x), ti, tj);
     const int64_t i0 = (int64_t)ti * kWideTile, j0 = (int64_t)tj * kWideTile;
@@ -17,9 +16,8 @@ __global__ __launch_bounds__(256) void grad_kernel(wide_args t)
     wide_steps(t, blockIdx.y % t.parts, first, last);
     f32x4 acc[8][8];
     wide_sums<KIND, false>(t, lds, i0, j0, out_of, first, last, acc);
-    fp8_matrix out = out_of ? t.out[1] : t.out[0];
-    if (t.parts > 1) out = fp8_matrix{t.work + (int64_t)blockIdx.y * t.rows * t.cols, PVQ_F32, t.cols};
-    store_fragments<8, 8>(out, t.vec, t.rows, t.cols, i0 + wave / 2 * 128, j0 + wave % 2 * 128, [&](int i, int j) { return read_sums(acc[i][j]); });
+    const fp8_matrix out = t.parts > 1 ? part_of(t.work, blockIdx.y, t.rows, t.cols) : out_of ? t.out[1] : t.out[0];
+    store_plain(out, t.rows, t.cols, lds, acc, i0, j0);
 }
 
 // the parts of the sum of an output's tiles
@@ -48,7 +46,6 @@ hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t
     t.work = g.work;
     t.parts = parts_of(t.rows, t.cols, t.depth, t.terms, outputs);
     t.steps_a_part = (int)(((t.depth + kWideStep - 1) / kWideStep * t.terms + t.parts - 1) / t.parts);
-    t.vec = t.parts > 1 ? (t.cols % 8 == 0 ? 8 : t.cols % 4 == 0 ? 4 : 1) : std::min(row_alignment(t.out[0]), outputs == 1 ? 8 : row_alignment(t.out[1]));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(t.tiles_i * t.tiles_j), (unsigned)(outputs * t.parts)), dim3(256), kWideLds, s, t);
     e = hipGetLastError();
     for (int i = 0; i < outputs && t.parts > 1 && e == hipSuccess; i++)

@@ -30,90 +30,83 @@ struct tile_args {
 
 // what becomes of a tile's sums
 struct tile_out {
-    fp8_matrix y;                // (data null: the gated block's result goes to hc, he alone)
-    int vec;                     // what y's rows are aligned to: 8 values, 4 or 1
-    int act;
-    uint8_t *hc, *he, *gc, *ge, *uc, *ue;
+    fp8_matrix y;                // of a product
+    gated_out gated;
     int parts;                   // of a split, whose sums go to work: [part][rows][n], GATED [part][G, U][rows][n]
     float *work;
 };
 
-// The sums of a tile at m0, n0 (GATED: of 128 hidden units), or what the gated block makes of them, to memory.  Four waves, 128 x 128 sums each.
+// The sums of a tile at m0, n0 (GATED: of 128 hidden units), or what the gated block makes of them, to memory.
 template <bool GATED>
 __device__ __forceinline__ void store_tile(const tile_out &t, int64_t rows, int64_t n, uint8_t *lds, const f32x4 (&acc)[8][8], int64_t m0, int64_t n0, int part)
 {
-    constexpr int F = 8, FH = GATED ? F / 2 : F;
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int wm = wave / 2, wn = wave % 2, r16 = lane % 16, quarter = lane / 16;
-    const int64_t row0 = m0 + wm * 128, col0 = n0 + wn * FH * 16;
-    auto sum = [&](int i, int j) { return read_sums(acc[i][j]); };
-    auto second = [&](int i, int j) { return read_sums(acc[i][j + F - FH]); };         // (GATED: U)
     const bool split = t.parts > 1;
-    const int split_vec = n % 8 == 0 ? 8 : n % 4 == 0 ? 4 : 1;
-    float *to = t.work + (int64_t)part * (GATED ? 2 : 1) * rows * n;
-    if constexpr (!GATED) store_fragments<F, F>(split ? fp8_matrix{to, PVQ_F32, n} : t.y, split ? split_vec : t.vec, rows, n, row0, col0, sum);
+    if constexpr (!GATED) store_plain(split ? part_of(t.work, part, rows, n) : t.y, rows, n, lds, acc, m0, n0);
     else {
-        if (split) {
-            store_fragments<F, FH>({to, PVQ_F32, n}, split_vec, rows, n, row0, col0, sum);
-            store_fragments<F, FH>({to + rows * n, PVQ_F32, n}, split_vec, rows, n, row0, col0, second);
-            return;
-        }
-        // (formed where it is wanted, twice for blocks: all of it at once would not fit beside the sums)
-        auto result = [&](int i, int j) {
-            f32x4 v = sum(i, j);
-            const f32x4 u = second(i, j);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, chunk = lane % 16 * 2;
+        const int64_t col = n0 + lane % 16 * 8;
+        store_rows(lds, acc, [&](int j) { return j / 4 * 128 + wave % 2 * 64 + j % 4 * 16; }, [&](int half, auto at) {
+            // sixteen lanes have the 128 hidden units of a row; a wave's rows four at a time, two times ahead
+            auto rows_of = [&](auto what) {
+#pragma unroll 1
+                for (int r0 = wave * 4 + lane / 16; r0 < 128; r0 += 32) {
+                    float g[2][8], u[2][8];
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = act_value(t.act, v[e]) * u[e];
-            return v;
-        };
-        if (t.y.data) store_fragments<F, FH>(t.y, t.vec, rows, n, row0, col0, result);
-        // to blocks: the tile's hidden units are one block, of which the two waves of a row of tiles hold a half each
-        const int64_t code_row = (n + kFp8Block - 1) / kFp8Block * kFp8Block, exp_row = (code_row / kFp8Block + 3) / 4 * 4, block = n0 / kFp8Block;
-        uint32_t *tops = reinterpret_cast<uint32_t *>(lds);          // [row of the tile][half]
-        auto to_blocks = [&](uint8_t *codes, uint8_t *exps, auto value) {
-            if (!codes) return;
-            __syncthreads();
+                    for (int k = 0; k < 2; k++)
 #pragma unroll
-            for (int i = 0; i < F; i++) {
-                uint32_t top = 0;
+                        for (int h = 0; h < 2; h++) {
+                            const f32x4 a = *at(r0 + 16 * k, chunk + h), b = *at(r0 + 16 * k, 32 + chunk + h);
 #pragma unroll
-                for (int j = 0; j < FH; j++) {
-                    const f32x4 v = value(i, j);
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (col0 + j * 16 + 4 * quarter + e < n) top = max(top, finite_bits(v[e]));
+                            for (int e = 0; e < 4; e++) { g[k][4 * h + e] = a[e]; u[k][4 * h + e] = b[e]; }
+                        }
+                    what(m0 + tile_row(half, r0), g[0], u[0], m0 + tile_row(half, r0 + 16), g[1], u[1]);
                 }
-                top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-                if (quarter == 0) tops[(wm * 128 + i * 16 + r16) * 2 + wn] = top;
+            };
+            const gated_out &o = t.gated;
+            const bool plain = o.h.data && !o.hc && !o.gc && o.h.dtype == PVQ_BF16 && n0 + 128 <= n;
+            // whole rows of H in bfloat16 alone, as a prompt wants them
+            auto prompt = [&](auto ACT) {
+                rows_of([&](int64_t row, float (&g)[8], float (&u)[8], int64_t next_row, float (&next_g)[8], float (&next_u)[8]) {
+                    u32x4 w[2];
+#pragma unroll
+                    for (int k = 0; k < 2; k++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const float *a = k ? next_g : g, *b = k ? next_u : u;
+                            w[k][e] = bf16_pair(act_value<decltype(ACT)::value>(a[2 * e]) * b[2 * e], act_value<decltype(ACT)::value>(a[2 * e + 1]) * b[2 * e + 1]);
+                        }
+                    uint16_t *h = reinterpret_cast<uint16_t *>(o.h.data) + col;
+                    if (row < rows) store_vector(h + row * o.h.ld, w[0]);
+                    if (next_row < rows) store_vector(h + next_row * o.h.ld, w[1]);
+                });
+            };
+            auto all = [&](auto ACT) {
+                rows_of([&](int64_t row, float (&g)[8], float (&u)[8], int64_t next_row, float (&next_g)[8], float (&next_u)[8]) {
+                    store_gated8<decltype(ACT)::value>(o, row, n, n0 / kFp8Block, col, row < rows, g, u);
+                    store_gated8<decltype(ACT)::value>(o, next_row, n, n0 / kFp8Block, col, next_row < rows, next_g, next_u);
+                });
+            };
+            if (split) {
+                // (G's columns and U's are two matrices)
+                const fp8_matrix to_g = part_of(t.work, 2 * part, rows, n), to_u = part_of(t.work, 2 * part + 1, rows, n);
+                rows_of([&](int64_t row, float (&g)[8], float (&u)[8], int64_t next_row, float (&next_g)[8], float (&next_u)[8]) {
+#pragma unroll 1
+                    for (int k = 0; k < 4; k++) {
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] = k == 0 ? g[e] : k == 1 ? u[e] : k == 2 ? next_g[e] : next_u[e];
+                        const int64_t r = k < 2 ? row : next_row;
+                        if (r < rows && col < n) store_values(k % 2 ? to_u : to_g, r, col, n - col, v);
+                    }
+                });
+            } else if (plain) {
+                if (o.act == PVQ_SILU) prompt(std::integral_constant<int, PVQ_SILU>{});
+                else prompt(std::integral_constant<int, PVQ_GELU>{});
+            } else {
+                if (o.act == PVQ_SILU) all(std::integral_constant<int, PVQ_SILU>{});
+                else all(std::integral_constant<int, PVQ_GELU>{});
             }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < F; i++) {
-                const int in = wm * 128 + i * 16 + r16;
-                const int64_t row = m0 + in;
-                const uint32_t e = exponent_of(max(tops[in * 2], tops[in * 2 + 1]));
-                const float inverse = scale_of(254 - e);
-#pragma unroll
-                for (int j = 0; j < FH; j++) {
-                    const int64_t col = col0 + j * 16 + 4 * quarter;
-                    f32x4 v = value(i, j);
-                    if (row >= rows) continue;
-#pragma unroll
-                    for (int q = 0; q < 4; q++) if (col + q >= n) v[q] = 0.0f;
-                    *reinterpret_cast<uint32_t *>(codes + row * code_row + col) = codes4(v[0], v[1], v[2], v[3], inverse);
-                }
-                if (row < rows && wn == 0 && quarter == 0) {
-                    uint8_t *p = exps + row * exp_row;
-                    p[block] = (uint8_t)e;
-                    if ((block + 1) * kFp8Block >= n)
-                        for (int64_t b = block + 1; b < exp_row; b++) p[b] = 0;
-                }
-            }
-        };
-        to_blocks(t.gc, t.ge, sum);
-        to_blocks(t.uc, t.ue, second);
-        to_blocks(t.hc, t.he, result);
+        });
     }
 }
 
@@ -330,7 +323,7 @@ size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide) { return work_
 hipError_t fp8_launch_product(const fp8_product_args &p, hipStream_t s)
 {
     tile_out out{};
-    out.y = p.y; out.vec = row_alignment(p.y); out.work = p.work;
+    out.y = p.y; out.work = p.work;
     hipError_t e = launch_tiles<false>(p.a, p.b, {}, out, p.y.dtype == PVQ_F32, s);
     if (out.parts > 1 && e == hipSuccess) e = fp8_launch_join(p.work, out.parts, p.a.rows, p.b.rows, p.y, s);
     return e;
@@ -339,8 +332,8 @@ hipError_t fp8_launch_product(const fp8_product_args &p, hipStream_t s)
 hipError_t fp8_launch_gated(const fp8_gated_args &g, hipStream_t s)
 {
     tile_out out{};
-    out.y = g.h; out.vec = row_alignment(g.h); out.act = g.act; out.work = g.work;
-    out.hc = g.hc; out.he = g.he; out.gc = g.gc; out.ge = g.ge; out.uc = g.uc; out.ue = g.ue;
+    out.gated = {g.h, g.act, g.hc, g.he, g.gc, g.ge, g.uc, g.ue};
+    out.work = g.work;
     // Kept products are codes of sums of 32 bits: what the 8-bit instructions are off would change one code of 2000, which is as
     // much again as the roundings of the gradients to bfloat16 (dX 3.0e-3 off instead of 2.3e-3).
     const bool wide = g.gc || (g.h.data && g.h.dtype == PVQ_F32);

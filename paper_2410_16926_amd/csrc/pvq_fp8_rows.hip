@@ -9,7 +9,6 @@ struct rows_args {
     fp8_blocks a, b, up;
     fp8_matrix y;
     int act;
-    bool vec;
 };
 
 // A workgroup takes 16 rows of the weights (of both of them, GATED) and 16 FM tokens; its waves take the blocks of 128 in
@@ -91,12 +90,12 @@ __global__ __launch_bounds__(512) void rows_kernel(rows_args t)
         f32x4 out = total[0];
         if constexpr (GATED) {
 #pragma unroll
-            for (int e = 0; e < 4; e++) out[e] = act_value(t.act, total[0][e]) * total[1][e];
+            for (int e = 0; e < 4; e++) out[e] = (t.act == PVQ_SILU ? act_value<PVQ_SILU>(total[0][e]) : act_value<PVQ_GELU>(total[0][e])) * total[1][e];
         }
         const int64_t row = m0 + 16 * j + r16, col = n0 + 4 * quarter;
         if (row < m) {
-            if (t.vec) store4<true>(t.y, row, col, n - col, out);
-            else store4<false>(t.y, row, col, n - col, out);
+            const float v[4] = {out[0], out[1], out[2], out[3]};
+            store_values(t.y, row, col, n - col, v);
         }
     }
 }
@@ -114,8 +113,6 @@ hipError_t launch_rows(const rows_args &t, hipStream_t s)
 template <bool GATED>
 hipError_t launch_rows_of(rows_args &t, hipStream_t s)
 {
-    const int size = t.y.dtype == PVQ_F32 ? 4 : 2;
-    t.vec = (uintptr_t)t.y.data % (4 * size) == 0 && t.y.ld % 4 == 0;
     if (t.a.rows <= 16) return launch_rows<1, GATED>(t, s);
     if (t.a.rows <= 32) return launch_rows<2, GATED>(t, s);
     return launch_rows<4, GATED>(t, s);

@@ -98,39 +98,85 @@ __device__ __forceinline__ void multiply_accumulated(f32x4 &c, bf16x8 a, bf16x8 
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
-// FM x FN fragments of 16 x 16 of a result to memory, from row0 and col0 on, rows and columns the result's.  A lane has four neighbouring columns of one
-// row: columns 4 (lane / 16 % 4) .. of a fragment, row lane % 16.  vec: what y's rows are aligned to, 8 values, 4 or 1.
-template <int FM, int FN, typename V>
-__device__ __forceinline__ void store_fragments(const fp8_matrix &y, int vec, int64_t rows, int64_t cols, int64_t row0, int64_t col0, V value)
+// The sums of a tile of 256 x 256 to its rows, by way of LDS (128 KB of it), which everybody has read and nobody loads into any more.  A lane has
+// four neighbouring columns of one row of a fragment: row lane % 16, columns 4 (lane / 16) ..; the rows are taken whole again, in short loops.  (The
+// first workgroups of a launch wait for each line of instructions: stored from where the sums are, unrolled over 64 fragments for every type and
+// alignment, that was 200 KB of them.)  column(j): where a wave's fragments j start.
+// rows(half, at): what becomes of the upper or the lower 64 rows of both waves that are side by side; at(r, chunk) is where four columns of the
+// half's row r are (row tile_row(half, r) of the tile).
+__device__ inline int tile_row(int half, int r) { return r / 64 * 128 + half * 64 + r % 64; }
+
+template <typename COLUMN, typename ROWS>
+__device__ __forceinline__ void store_rows(uint8_t *lds, const f32x4 (&acc)[8][8], COLUMN column, ROWS rows)
 {
-    const int lane = threadIdx.x % kWave, r16 = lane % 16, quarter = lane / 16;
-    if (vec == 8 && row0 + FM * 16 <= rows && col0 + FN * 16 <= cols) {
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave / 2, r16 = lane % 16, quarter = lane / 16;
+    // row r of 256 columns, a KiB in 64 chunks of four; chunk c lies at place c ^ (r % 16)
+    auto at = [&](int r, int chunk) { return reinterpret_cast<f32x4 *>(lds + r * 1024 + ((chunk ^ (r & 15)) << 4)); };
 #pragma unroll
-        for (int i = 0; i < FM; i++)
+    for (int half = 0; half < 2; half++) {
+        all_reads();                                     // (not the stores, as __syncthreads would)
+        barrier();
 #pragma unroll
-            for (int j = 0; j < FN; j += 2) store_pair(y, row0 + i * 16 + r16, col0 + j * 16, quarter, value(i, j), value(i, j + 1));
-        return;
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) *at(wm * 64 + i * 16 + r16, column(j) / 4 + quarter) = read_sums(acc[half * 4 + i][j]);
+        all_reads();
+        barrier();
+        rows(half, at);
     }
+}
+
+// Eight columns a lane, where all of them are inside: a wave two rows at a time, four times ahead.
+template <int T, typename AT>
+__device__ __forceinline__ void store_whole(const fp8_matrix &y, int64_t row0, int64_t rows, int64_t col, bool there, int half, AT at)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, chunk = lane % 32 * 2;
+#pragma unroll 1
+    for (int r0 = wave * 2 + lane / 32; r0 < 128; r0 += 32) {
+        f32x4 lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < FM; i++) {
-        const int64_t row = row0 + i * 16 + r16;
+        for (int k = 0; k < 4; k++) { lo[k] = *at(r0 + 8 * k, chunk); hi[k] = *at(r0 + 8 * k, chunk + 1); }
 #pragma unroll
-        for (int j = 0; j < FN; j++) {
-            const int64_t col = col0 + j * 16 + 4 * quarter;
-            const f32x4 v = value(i, j);
-            if (row >= rows) continue;
-            if (vec >= 4) store4<true>(y, row, col, cols - col, v);
-            else store4<false>(y, row, col, cols - col, v);
+        for (int k = 0; k < 4; k++) {
+            const int64_t row = row0 + tile_row(half, r0 + 8 * k), to = row * y.ld + col;
+            if (!there || row >= rows) continue;
+            if constexpr (T == PVQ_F32) {
+                store_vector(reinterpret_cast<float *>(y.data) + to, lo[k]);
+                store_vector(reinterpret_cast<float *>(y.data) + to + 4, hi[k]);
+            } else {
+                auto pair = [](float a, float b) { return T == PVQ_BF16 ? bf16_pair(a, b) : f16_pair(a, b); };
+                store_vector(reinterpret_cast<uint16_t *>(y.data) + to, u32x4{pair(lo[k][0], lo[k][1]), pair(lo[k][2], lo[k][3]), pair(hi[k][0], hi[k][1]), pair(hi[k][2], hi[k][3])});
+            }
         }
     }
 }
 
-inline int row_alignment(const fp8_matrix &y)
+// ... to a matrix, the tile's first element at row0, col0
+__device__ __forceinline__ void store_plain(const fp8_matrix &y, int64_t rows, int64_t cols, uint8_t *lds, const f32x4 (&acc)[8][8], int64_t row0, int64_t col0)
 {
-    const int size = y.dtype == PVQ_F32 ? 4 : 2;
-    for (const int n : {8, 4})
-        if ((uintptr_t)y.data % std::min(16, n * size) == 0 && y.ld % n == 0) return n;
-    return 1;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int64_t col = col0 + lane % 32 * 8;
+    store_rows(lds, acc, [&](int j) { return wave % 2 * 128 + j * 16; }, [&](int half, auto at) {
+        const bool whole = col + 8 <= cols;
+        if (y.dtype == PVQ_F32) store_whole<PVQ_F32>(y, row0, rows, col, whole, half, at);
+        else if (y.dtype == PVQ_BF16) store_whole<PVQ_BF16>(y, row0, rows, col, whole, half, at);
+        else store_whole<PVQ_F16>(y, row0, rows, col, whole, half, at);
+        // what is left of the rows behind their last eight: a row a lane
+        const int left = (int)(cols % 8);
+        const int64_t from = cols - left - col0, row = row0 + tile_row(half, threadIdx.x % 128);
+        if (left == 0 || from >= 256 || threadIdx.x >= 128 || row >= rows) return;
+#pragma unroll 1
+        for (int e = 0; e < left; e++) {
+            const float v = reinterpret_cast<const float *>(at(threadIdx.x, (int)(from + e) / 4))[(from + e) % 4];
+            const int64_t to = row * y.ld + col0 + from + e;
+            if (y.dtype == PVQ_F32) reinterpret_cast<float *>(y.data)[to] = v;
+            else reinterpret_cast<uint16_t *>(y.data)[to] = (uint16_t)(y.dtype == PVQ_BF16 ? bf16_pair(v, v) : f16_pair(v, v));
+        }
+    });
 }
+
+// ... a split's, rows of `cols` sums without a gap
+__device__ __forceinline__ fp8_matrix part_of(float *work, int64_t part, int64_t rows, int64_t cols) { return {work + part * rows * cols, PVQ_F32, cols}; }
 
 }  // namespace pvq_fp8_dev

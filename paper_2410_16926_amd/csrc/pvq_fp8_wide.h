@@ -24,7 +24,6 @@ struct wide_args {
     int tiles_i, tiles_j;
     int parts, steps_a_part;         // of a split sum, whose parts go to work
     float *work;
-    int vec;                         // what the outputs' rows are aligned to: 8 values, 4 or 1
 };
 
 // Steps first .. last of the tile at i0, j0.  Four waves of 128 x 128, one to a SIMD, as for products on the 8-bit instruction
@@ -184,10 +183,24 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     };
     if (first > last) { sums_are_there(); return; }
     start(first);
-    fetch_all(first);
-    put_all(0);
-    fetch_all(first + 1);
-    put_all(kPlane);
+    {
+        // (the second step's on its way while the first is waited for)
+        u32x4 a[2][kPieces];
+        u32x2 b[2][kPieces];
+        uint32_t e[2][kPieces];
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            fetch_all(first + s);
+#pragma unroll
+            for (int p = 0; p < kPieces; p++) { a[s][p] = ra[p]; b[s][p] = rb[p]; e[s][p] = re[p]; }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+#pragma unroll
+            for (int p = 0; p < kPieces; p++) { ra[p] = a[s][p]; rb[p] = b[s][p]; re[p] = e[s][p]; }
+            put_all(s * kPlane);
+        }
+    }
     fetch_all(first + 2);
     all_reads();
     barrier();
