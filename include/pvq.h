@@ -347,7 +347,7 @@ int pvq_fp8_decode(const uint8_t *codes, const uint8_t *exponents, int64_t rows,
  * Y = A B^T, A [m][k] and B [n][k] in blocks, Y [m][ldy] of out_dtype: tokens times weights, any number of tokens.
  * Sums are float32.  To PVQ_F32 they are formed of the decoded values by the bfloat16 matrix instructions; to PVQ_BF16 and PVQ_F16
  * by the 8-bit ones, which align the products of a group of eight to the largest among them and drop what lies 14 bits below
- * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 64) take the
+ * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 32) take the
  * bfloat16 instructions for every type.  The order of the sums depends on the shape alone.
  *   work   device, 16-byte aligned scratch of pvq_fp8_product_work_bytes bytes (may be NULL where that is 0); calls that
  *          may overlap in time need one each
