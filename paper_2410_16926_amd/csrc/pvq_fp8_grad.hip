@@ -9,15 +9,11 @@ template <int KIND>
 __global__ __launch_bounds__(256) void grad_kernel(wide_args t)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    int ti, tj, first, last;
-    tile_of(t.tiles_i, t.tiles_j, chiplet_order(blockIdx.x, gridDim.x), ti, tj);
-    const int64_t i0 = (int64_t)ti * kWideTile, j0 = (int64_t)tj * kWideTile;
-    const int out_of = blockIdx.y / t.parts;
-    wide_steps(t, blockIdx.y % t.parts, first, last);
-    f32x4 acc[8][8];
-    wide_sums<KIND, false>(t, lds, i0, j0, out_of, first, last, acc);
-    const fp8_matrix out = t.parts > 1 ? part_of(t.work, blockIdx.y, t.rows, t.cols) : out_of ? t.out[1] : t.out[0];
-    store_plain(out, t.rows, t.cols, lds, acc, i0, j0);
+    wide_sums<KIND, false>(t, lds, t.units, [&](int u) { return wide_unit_of<false>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[8][8]) {
+        const wide_args &t = argument<wide_args>();
+        const fp8_matrix out = t.parts > 1 ? part_of(t.work, u.out_of * t.parts + u.part, t.rows, t.cols) : u.out_of ? t.out[1] : t.out[0];
+        store_sums(out, t.rows, t.cols, acc, u.i0, u.j0);
+    });
 }
 
 // the parts of the sum of an output's tiles
@@ -46,7 +42,8 @@ hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t
     t.work = g.work;
     t.parts = parts_of(t.rows, t.cols, t.depth, t.terms, outputs);
     t.steps_a_part = (int)(((t.depth + kWideStep - 1) / kWideStep * t.terms + t.parts - 1) / t.parts);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(t.tiles_i * t.tiles_j), (unsigned)(outputs * t.parts)), dim3(256), kWideLds, s, t);
+    t.units = t.tiles_i * t.tiles_j * outputs * t.parts;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(t.units, 256)), dim3(256), kWideLds, s, t);
     e = hipGetLastError();
     for (int i = 0; i < outputs && t.parts > 1 && e == hipSuccess; i++)
         e = fp8_launch_join(t.work + (int64_t)i * t.parts * t.rows * t.cols, t.parts, t.rows, t.cols, t.out[i], s);

@@ -41,7 +41,7 @@ template <bool GATED>
 __device__ __forceinline__ void store_tile(const tile_out &t, int64_t rows, int64_t n, uint8_t *lds, const f32x4 (&acc)[8][8], int64_t m0, int64_t n0, int part)
 {
     const bool split = t.parts > 1;
-    if constexpr (!GATED) store_plain(split ? part_of(t.work, part, rows, n) : t.y, rows, n, lds, acc, m0, n0);
+    if constexpr (!GATED) store_sums(split ? part_of(t.work, part, rows, n) : t.y, rows, n, acc, m0, n0);
     else {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, chunk = lane % 16 * 2;
         const int64_t col = n0 + lane % 16 * 8;
@@ -265,13 +265,10 @@ template <bool GATED>
 __global__ __launch_bounds__(256) void wide_tile_kernel(wide_args t, tile_out out)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    int ti, tj, first, last;
-    tile_of(t.tiles_i, t.tiles_j, chiplet_order(blockIdx.x, gridDim.x), ti, tj);
-    const int64_t i0 = (int64_t)ti * kWideTile, j0 = (int64_t)tj * (GATED ? kWideTile / 2 : kWideTile);
-    wide_steps(t, blockIdx.y, first, last);
-    f32x4 acc[8][8];
-    wide_sums<WIDE_PRODUCT, GATED>(t, lds, i0, j0, 0, first, last, acc);
-    store_tile<GATED>(out, t.rows, t.cols, lds, acc, i0, j0, blockIdx.y);
+    wide_sums<WIDE_PRODUCT, GATED>(t, lds, t.units, [&](int u) { return wide_unit_of<GATED>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[8][8]) {
+        const wide_args &t = argument<wide_args>();
+        store_tile<GATED>(argument<tile_out>(sizeof(wide_args)), t.rows, t.cols, lds, acc, u.i0, u.j0, u.part);
+    });
 }
 
 int64_t tiles_of(int64_t m, int64_t n, bool gated) { return ((m + 255) / 256) * ((n + (gated ? 127 : 255)) / (gated ? 128 : 256)); }
@@ -305,7 +302,8 @@ hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_bloc
         t.rows = m; t.cols = n; t.depth = k; t.terms = 1; t.parts = out.parts;
         t.tiles_i = (int)((m + 255) / 256); t.tiles_j = (int)(grid.x / t.tiles_i);
         t.steps_a_part = (int)(((k + kWideStep - 1) / kWideStep + t.parts - 1) / t.parts);
-        hipLaunchKernelGGL(wide_tile_kernel<GATED>, grid, dim3(256), kWideLds, s, t, out);
+        t.units = (int)(grid.x * grid.y);
+        hipLaunchKernelGGL(wide_tile_kernel<GATED>, dim3((unsigned)(GATED ? t.units : std::min(t.units, 256))), dim3(256), kWideLds, s, t, out);
     } else {
         tile_args t{a, b, up, n, (int)((m + 255) / 256), 0, 0};
         t.tiles_n = (int)(grid.x / t.tiles_m);

@@ -98,6 +98,27 @@ __device__ __forceinline__ void multiply_accumulated(f32x4 &c, bf16x8 a, bf16x8 
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
+// A kernel's argument that starts at byte `offset` of them, read anew: kept in scalar registers for what happens once a tile, arguments leave too few
+// of them to the steps.
+template <typename T>
+__device__ __forceinline__ const T &argument(int offset = 0)
+{
+    auto p = (const __attribute__((address_space(4))) uint8_t *)(uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const T *)(p + offset);
+}
+
+// All sums zero, where they are.
+__device__ __forceinline__ void no_sums(f32x4 (&acc)[8][8])
+{
+    u32x4 zero{0, 0, 0, 0};
+    asm volatile("s_nop 7" : "+v"(zero));                // (written, and some instructions before the first below)
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %1, 0" : "+a"(acc[i][j]) : "v"(zero));
+}
+
 // The sums of a tile of 256 x 256 to its rows, by way of LDS (128 KB of it), which everybody has read and nobody loads into any more.  A lane has
 // four neighbouring columns of one row of a fragment: row lane % 16, columns 4 (lane / 16) ..; the rows are taken whole again, in short loops.  (The
 // first workgroups of a launch wait for each line of instructions: stored from where the sums are, unrolled over 64 fragments for every type and
@@ -127,53 +148,79 @@ __device__ __forceinline__ void store_rows(uint8_t *lds, const f32x4 (&acc)[8][8
     }
 }
 
-// Eight columns a lane, where all of them are inside: a wave two rows at a time, four times ahead.
-template <int T, typename AT>
-__device__ __forceinline__ void store_whole(const fp8_matrix &y, int64_t row0, int64_t rows, int64_t col, bool there, int half, AT at)
+// A tile's sums to a matrix, the tile's first at row0, col0, from where they are: LDS may hold the next tile's operands by now.  Four waves of 128 x 128;
+// a lane has four neighbouring columns of one row of a fragment.  float32 is stored so, 16 rows of 64 bytes at a time.  Of 16-bit types two fragments'
+// halves and quarters change places, after which a lane has eight neighbouring columns: 64 bytes of a row again.  (Every sum is read at one place,
+// whatever the type: of reads in several branches the compiler moves some up, to where the sums need not be there yet.)
+__device__ __forceinline__ void store_sums(const fp8_matrix &y, int64_t rows, int64_t cols, const f32x4 (&acc)[8][8], int64_t row0, int64_t col0)
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, chunk = lane % 32 * 2;
-#pragma unroll 1
-    for (int r0 = wave * 2 + lane / 32; r0 < 128; r0 += 32) {
-        f32x4 lo[4], hi[4];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
+    row0 += wave / 2 * 128;
+    col0 += wave % 2 * 128;
+    const bool inside = row0 + 128 <= rows && col0 + 128 <= cols, f32 = y.dtype == PVQ_F32, bf16 = y.dtype == PVQ_BF16;
+    const int bytes = f32 ? 4 : 2;
+    const int64_t row = row0 + r16, col = col0 + quarter * (f32 ? 4 : 8);
+    uint8_t *to = reinterpret_cast<uint8_t *>(y.data) + (row * y.ld + col) * bytes;
 #pragma unroll
-        for (int k = 0; k < 4; k++) { lo[k] = *at(r0 + 8 * k, chunk); hi[k] = *at(r0 + 8 * k, chunk + 1); }
+    for (int i = 0; i < 8; i++, to += 16 * y.ld * bytes) {
+        const bool there = row + 16 * i < rows;
+        const int64_t left = there ? cols - col : 0;
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 s[8];
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const int64_t row = row0 + tile_row(half, r0 + 8 * k), to = row * y.ld + col;
-            if (!there || row >= rows) continue;
-            if constexpr (T == PVQ_F32) {
-                store_vector(reinterpret_cast<float *>(y.data) + to, lo[k]);
-                store_vector(reinterpret_cast<float *>(y.data) + to + 4, hi[k]);
-            } else {
-                auto pair = [](float a, float b) { return T == PVQ_BF16 ? bf16_pair(a, b) : f16_pair(a, b); };
-                store_vector(reinterpret_cast<uint16_t *>(y.data) + to, u32x4{pair(lo[k][0], lo[k][1]), pair(lo[k][2], lo[k][3]), pair(hi[k][0], hi[k][1]), pair(hi[k][2], hi[k][3])});
+        for (int j = 0; j < 8; j++) s[j] = read_sums(acc[i][j]);
+        if (f32) {
+            float *at = reinterpret_cast<float *>(to);
+            if (__builtin_expect(inside, 1)) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) store_vector(at + 16 * j, s[j]);
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                if (left >= 16 * j + 4) store_vector(at + 16 * j, s[j]);
+                else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (16 * j + e < left) at[16 * j + e] = s[j][e];
+                }
+            }
+            continue;
+        }
+        uint32_t w[8][2];
+        if (bf16) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) { w[j][0] = bf16_pair(s[j][0], s[j][1]); w[j][1] = bf16_pair(s[j][2], s[j][3]); }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) { w[j][0] = f16_pair(s[j][0], s[j][1]); w[j][1] = f16_pair(s[j][2], s[j][3]); }
+        }
+        u32x4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const auto halves = __builtin_amdgcn_permlane32_swap(w[2 * j][e], w[2 * j + 1][e], false, false);
+                const auto quarters = __builtin_amdgcn_permlane16_swap(halves[0], halves[1], false, false);
+                v[j][e] = quarters[0];
+                v[j][2 + e] = quarters[1];
+            }
+        uint16_t *at = reinterpret_cast<uint16_t *>(to);
+        if (__builtin_expect(inside, 1)) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) store_vector(at + 32 * j, v[j]);
+            continue;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            if (left >= 32 * j + 8) store_vector(at + 32 * j, v[j]);
+            else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (32 * j + e < left) at[32 * j + e] = (uint16_t)(v[j][e / 2] >> 16 * (e % 2));
             }
         }
     }
-}
-
-// ... to a matrix, the tile's first element at row0, col0
-__device__ __forceinline__ void store_plain(const fp8_matrix &y, int64_t rows, int64_t cols, uint8_t *lds, const f32x4 (&acc)[8][8], int64_t row0, int64_t col0)
-{
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int64_t col = col0 + lane % 32 * 8;
-    store_rows(lds, acc, [&](int j) { return wave % 2 * 128 + j * 16; }, [&](int half, auto at) {
-        const bool whole = col + 8 <= cols;
-        if (y.dtype == PVQ_F32) store_whole<PVQ_F32>(y, row0, rows, col, whole, half, at);
-        else if (y.dtype == PVQ_BF16) store_whole<PVQ_BF16>(y, row0, rows, col, whole, half, at);
-        else store_whole<PVQ_F16>(y, row0, rows, col, whole, half, at);
-        // what is left of the rows behind their last eight: a row a lane
-        const int left = (int)(cols % 8);
-        const int64_t from = cols - left - col0, row = row0 + tile_row(half, threadIdx.x % 128);
-        if (left == 0 || from >= 256 || threadIdx.x >= 128 || row >= rows) return;
-#pragma unroll 1
-        for (int e = 0; e < left; e++) {
-            const float v = reinterpret_cast<const float *>(at(threadIdx.x, (int)(from + e) / 4))[(from + e) % 4];
-            const int64_t to = row * y.ld + col0 + from + e;
-            if (y.dtype == PVQ_F32) reinterpret_cast<float *>(y.data)[to] = v;
-            else reinterpret_cast<uint16_t *>(y.data)[to] = (uint16_t)(y.dtype == PVQ_BF16 ? bf16_pair(v, v) : f16_pair(v, v));
-        }
-    });
 }
 
 // ... a split's, rows of `cols` sums without a gap

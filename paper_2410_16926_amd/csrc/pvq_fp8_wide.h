@@ -23,10 +23,18 @@ struct wide_args {
     int terms;                       // of the sum
     int tiles_i, tiles_j;
     int parts, steps_a_part;         // of a split sum, whose parts go to work
+    int units;                       // tiles of all parts of all outputs
     float *work;
 };
 
-// Steps first .. last of the tile at i0, j0.  Four waves of 128 x 128, one to a SIMD, as for products on the 8-bit instruction
+// A tile, or a part of its sum: steps first .. last of output out_of at i0, j0.
+struct wide_unit {
+    int64_t i0, j0;
+    int out_of, part, first, last;
+    __device__ int steps() const { return max(last - first + 1, 1); }       // (of none: one of zeros)
+};
+
+// The sums of a workgroup's units, t the kernel's first argument, and what becomes of each: done(unit, acc).  Four waves of 128 x 128, one to a SIMD, as for products on the 8-bit instruction
 // (pvq_fp8_product.hip): LDS is written 64 KB and read 128 KB for 64 of the sum, 1500 of the 2048 cycles of matrix instructions.  Both operands come
 // through registers, codes to be decoded once for the four waves, dY as it is.
 //
@@ -34,11 +42,16 @@ struct wide_args {
 // stage; behind the step's barrier, while the second half's run, the next step's first operands are read from the other stage, then what was fetched
 // a step ago is put into the empty one.  One operand's codes are decoded in the first half, the other's in the second, and either is fetched again as
 // soon as its registers are free: a wave alone on its SIMD has about three instructions to issue beside each matrix instruction, and what does not fit
-// holds the next one up (all of it in the second half: 478 us for dX of 2048 x 2 x 14336 x 4096).
+// holds the next one up (all of it in the second half: 478 us for dX of 2048 x 2 x 14336 x 4096, now 420; where the loads are, worked out in one place
+// at the start of a step: 10 % more).
 //
 // GATED (WIDE_PRODUCT): the tile's 256 columns are 128 hidden units of the gate weights and the same of the up weights; a wave has both for its 64.
-template <int KIND, bool GATED>
-__device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int64_t i0, int64_t j0, int out_of, int first, int last, f32x4 (&acc)[8][8])
+//
+// A workgroup has units blockIdx.x, blockIdx.x + gridDim.x .. and goes from one to the next without a pause: three steps ahead of the products, its loads
+// are the next unit's when one ends, and between two steps the sums are stored from where they are.  (GATED: one unit, and done may use LDS.)
+// dW of 64 x 16384 x 4096, four tiles of one step to a workgroup, 38 us; with a workgroup to each tile, stored by way of LDS, 50; 576 tokens 85 and 97.
+template <int KIND, bool GATED, typename UNIT, typename DONE>
+__device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int units, UNIT unit_of, DONE done)
 {
     constexpr int F = 8, kPlane = kWideTile * kWideStep * 2, kPieces = 8;       // LDS: A's two stages, B's two stages
     constexpr bool A_ALONG = KIND != WIDE_WEIGHT_GRAD, B_ALONG = KIND == WIDE_PRODUCT, A_CODES = KIND == WIDE_PRODUCT;
@@ -60,56 +73,86 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     u32x2 rb[kPieces];
     uint32_t re[kPieces];
     bf16x8 decoded[kPieces];         // A's codes, or else B's, for the next half
-    // Where a step's part of an operand's tile starts, and how much of the matrix is left there: what lies behind, and everything of a step
-    // behind the last, is zero.
+    // Where a step's part of an operand's tile starts, and how many bytes of the matrix are left there, the upper word below zero where none are: what
+    // lies behind is zero.  (Of 64 bits compared whole the vector unit does it, between matrix instructions.)
     struct source {
         const uint8_t *p;
-        int64_t left, step;          // step: bytes to the next step
+        uint32_t left;
+        int32_t left_up;
     };
-    auto source_of = [](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at, int64_t step) {
-        return source{(const uint8_t *)base + at, (rows - 1) * row + row_bytes - at, step};
+    auto source_of = [](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at) {
+        const int64_t left = (rows - 1) * row + row_bytes - at;
+        return source{(const uint8_t *)base + at, (uint32_t)left, (int32_t)(left >> 32)};
     };
     source a_src, b_src, u_src, ae_src, be_src, ue_src;
-    auto start = [&](int step) {                  // at the first step, and where the second term begins
+    auto stop = [&] { a_src.left_up = b_src.left_up = u_src.left_up = ae_src.left_up = be_src.left_up = ue_src.left_up = -1; };
+    // where the loads are
+    wide_unit ahead = unit_of(blockIdx.x);
+    int ahead_u = blockIdx.x, step = ahead.first, ahead_left = 0;      // (steps to the end of the unit or its first term)
+    auto start = [&] {                  // at the first step, and where the second term begins
+        const wide_args &t = argument<wide_args>();
         const int term = step >= steps_a_term ? 1 : 0;
-        const bool second = (term | out_of) != 0;
+        const bool second = (term | ahead.out_of) != 0;
+        const int64_t i0 = ahead.i0, j0 = ahead.j0;
         const int64_t r0 = (int64_t)(step - term * steps_a_term) * kWideStep;
         const fp8_blocks b = {second ? t.b[1].codes : t.b[0].codes, second ? t.b[1].exps : t.b[0].exps, 0, 0};
         if constexpr (A_CODES) {
-            a_src = source_of(t.a.codes, a_row, t.rows, a_row, i0 * a_row + r0, kWideStep);
-            ae_src = source_of(t.a.exps, ae_row, t.rows, ae_row, i0 * ae_row, 0);
+            a_src = source_of(t.a.codes, a_row, t.rows, a_row, i0 * a_row + r0);
+            ae_src = source_of(t.a.exps, ae_row, t.rows, ae_row, i0 * ae_row + step / 2);
         } else {
             // (dY's last row to the end of its last 16 bytes: a load that is not whole would bring nothing)
             const int64_t row_end = ((A_ALONG ? (t.depth + kWideStep - 1) / kWideStep * kWideStep : t.rows) * 2 + 15) / 16 * 16;
             const uint16_t *y = second ? t.dy[1].data : t.dy[0].data;
-            a_src = A_ALONG ? source_of(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2, kWideStep * 2) : source_of(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2, (int64_t)kWideStep * a_row);
+            a_src = A_ALONG ? source_of(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2) : source_of(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2);
         }
         if constexpr (B_ALONG) {
-            b_src = source_of(t.b[0].codes, b_row, t.cols, b_row, j0 * b_row + r0, kWideStep);
-            be_src = source_of(t.b[0].exps, be_row, t.cols, be_row, j0 * be_row, 0);
-            u_src = GATED ? source_of(t.b[1].codes, b_row, t.cols, b_row, j0 * b_row + r0, kWideStep) : b_src;
-            ue_src = GATED ? source_of(t.b[1].exps, be_row, t.cols, be_row, j0 * be_row, 0) : be_src;
+            b_src = source_of(t.b[0].codes, b_row, t.cols, b_row, j0 * b_row + r0);
+            be_src = source_of(t.b[0].exps, be_row, t.cols, be_row, j0 * be_row + step / 2);
+            u_src = GATED ? source_of(t.b[1].codes, b_row, t.cols, b_row, j0 * b_row + r0) : b_src;
+            ue_src = GATED ? source_of(t.b[1].exps, be_row, t.cols, be_row, j0 * be_row + step / 2) : be_src;
         } else {
-            b_src = source_of(b.codes, b_row, t.depth, b_row, r0 * b_row + j0, (int64_t)kWideStep * b_row);
-            be_src = source_of(b.exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block, (int64_t)kWideStep * be_row);
+            b_src = source_of(b.codes, b_row, t.depth, b_row, r0 * b_row + j0);
+            be_src = source_of(b.exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block);
         }
+        if (step > ahead.last) stop();
+        ahead_left = max((KIND == WIDE_INPUT_GRAD && !term ? min(steps_a_term, ahead.last + 1) : ahead.last + 1) - step, 1);
     };
     __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
-    auto take = [&](source &s, int step, int64_t more = 0) {       // the buffer of a step, and on to the next
-        const int64_t left = step <= last ? min(s.left - more, (int64_t)0xFFFFFFFF) : 0;
-        const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)(s.p + more), 0, (uint32_t)(left < 0 ? 0 : left), 0x00020000);
-        s.p += s.step;
-        s.left -= s.step;
+    auto take = [](source &s, uint32_t step) {       // the buffer of a step, and on to the next, `step` bytes on
+        asm("" : "+s"(s.left_up));
+        const uint32_t left = s.left_up > 0 ? ~0u : s.left_up < 0 ? 0u : s.left;
+        const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, left, 0x00020000);
+        s.p += step;
+        s.left_up -= s.left < step;
+        s.left -= step;
         return r;
     };
-    auto aim = [&](int step) {
-        if (KIND == WIDE_INPUT_GRAD && step == steps_a_term) start(step);
-        // (rows along the sum: an exponent is that of two steps)
-        a_from = take(a_src, step);
-        if constexpr (A_CODES) ae_from = take(ae_src, step, step / 2);
-        b_from = take(b_src, step);
-        be_from = take(be_src, step, B_ALONG ? step / 2 : 0);
-        if constexpr (GATED) { u_from = take(u_src, step); ue_from = take(ue_src, step, step / 2); }
+    // (rows along the sum: an exponent is that of two steps)
+    const uint32_t a_step = A_CODES ? kWideStep : A_ALONG ? kWideStep * 2 : kWideStep * a_row, b_step = B_ALONG ? kWideStep : kWideStep * b_row;
+    auto aim_a = [&](int what) {
+        if (what == 0) a_from = take(a_src, a_step);
+        if (what == 1 && A_CODES) ae_from = take(ae_src, step & 1);
+    };
+    auto aim_b = [&](int what) {
+        if (what == 0) b_from = take(b_src, b_step);
+        if (what == 1) be_from = take(be_src, B_ALONG ? step & 1 : kWideStep * be_row);
+        if (what == 2 && GATED) u_from = take(u_src, b_step);
+        if (what == 3 && GATED) ue_from = take(ue_src, step & 1);
+    };
+    auto go_on = [&](int steps) {                 // behind so many; on to the second term or the next unit; behind the last unit there are steps of zeros
+        ahead_left -= steps;
+        if (ahead_left) return;
+        if (step > ahead.last) {
+            ahead_u += gridDim.x;
+            if (GATED || ahead_u >= units) {
+                stop();
+                ahead_left = 1 << 30;
+                return;
+            }
+            ahead = unit_of(ahead_u);
+            step = ahead.first;
+        }
+        start();
     };
     auto fetch_a = [&](int p) {
         if constexpr (A_CODES) {
@@ -131,7 +174,6 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
     const uint32_t across_to = across_row * 512 + (((across_col / 16) ^ (across_row & 3)) << 5) + across_col % 16 * 2, across_odd = across_to ^ (4 << 5);
     const uint32_t along_to = along_row * 128 + (((along_col / 8) ^ (along_row / 2 & 7)) << 4);
     auto place = [&](bool along, int p) { return p * 4096 + (along ? along_to : p & 1 ? across_odd : across_to); };
-    // (stages by the offset of their planes, 0 or kPlane: one body for all steps, whose sums stay where they are)
     auto decode = [&](int p) {
         if constexpr (A_CODES) decoded[p] = bf16x8_of_codes(ra[p][0], ra[p][1], scale_of(ra[p][2]));
         else decoded[p] = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
@@ -161,28 +203,25 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
         return B_ALONG ? read_along(stage + 2 * kPlane, GATED ? (j / 4) * 128 + wj * 64 + (j % 4) * 16 : wj * 128 + j * 16, h) : read_across(stage + 2 * kPlane, wj * 8 + j, h);
     };
 
-#pragma unroll
-    for (int i = 0; i < F; i++)
-#pragma unroll
-        for (int j = 0; j < F; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[F][F];
     bf16x8 a_op[2][F], b_op[2][F];
 
-    auto fetch_all = [&](int step) {
-        aim(step);
+    auto fetch_all = [&] {
+#pragma unroll
+        for (int i = 0; i < 4; i++) { aim_a(i); aim_b(i); }
+        step++;
+        go_on(1);
 #pragma unroll
         for (int p = 0; p < kPieces; p++) { fetch_a(p); fetch_b(p); }
-    };
-    auto put_all = [&](uint32_t stage) {
-#pragma unroll
-        for (int p = 0; p < kPieces; p++) { decode(p); put_a(stage, p); put_b(stage, p); }
     };
     // the reads of a half's operands behind its predecessor's first 32 instructions
     auto read_behind = [&](uint32_t stage, int slot, int h) {
         if (slot % 2 == 0 && slot / 2 < F) b_op[h][slot / 2] = read_b(stage, slot / 2, h);
         if (slot % 2 == 0 && slot / 2 >= F && slot / 2 < 2 * F) a_op[h][slot / 2 - F] = read_a(stage, slot / 2 - F, h);
     };
-    if (first > last) { sums_are_there(); return; }
-    start(first);
+    wide_unit now = ahead;
+    int u = blockIdx.x, left = now.steps();
+    start();
     {
         // (the second step's on its way while the first is waited for)
         u32x4 a[2][kPieces];
@@ -190,71 +229,103 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int6
         uint32_t e[2][kPieces];
 #pragma unroll
         for (int s = 0; s < 2; s++) {
-            fetch_all(first + s);
+            fetch_all();
 #pragma unroll
             for (int p = 0; p < kPieces; p++) { a[s][p] = ra[p]; b[s][p] = rb[p]; e[s][p] = re[p]; }
         }
 #pragma unroll
         for (int s = 0; s < 2; s++) {
 #pragma unroll
-            for (int p = 0; p < kPieces; p++) { ra[p] = a[s][p]; rb[p] = b[s][p]; re[p] = e[s][p]; }
-            put_all(s * kPlane);
+            for (int p = 0; p < kPieces; p++) { ra[p] = a[s][p]; rb[p] = b[s][p]; re[p] = e[s][p]; decode(p); put_a(s * kPlane, p); put_b(s * kPlane, p); }
         }
     }
-    fetch_all(first + 2);
+    fetch_all();
     all_reads();
     barrier();
 #pragma unroll
     for (int j = 0; j < F; j++) b_op[0][j] = read_b(0, j, 0);
 #pragma unroll
     for (int i = 0; i < F; i++) a_op[0][i] = read_a(0, i, 0);
+    no_sums(acc);
+    // (stages by the offset of their planes, 0 or kPlane: one body for all steps, whose sums stay where they are)
+    // In runs without a condition, until either the products or the loads come to an end of theirs.
     uint32_t stage = 0;
-    for (int step = first; step <= last; step++, stage ^= kPlane) {
-        aim(step + 3);
+    for (;;) {
+        const int run = min(left, ahead_left);
+        int more = run;
+        do {
 #pragma unroll
-        for (int i = 0; i < F; i++)
+            for (int i = 0; i < F; i++)
 #pragma unroll
-            for (int j = 0; j < F; j++) {
-                multiply_accumulated(acc[i][j], b_op[0][j], a_op[0][i]);
-                const int slot = i * F + j;
-                read_behind(stage, slot, 1);
-                if (slot >= 32 && slot % 4 == 1) {
-                    decode((slot - 32) / 4);
-                    if (A_CODES) fetch_a((slot - 32) / 4);
-                    else fetch_b((slot - 32) / 4);
+                for (int j = 0; j < F; j++) {
+                    multiply_accumulated(acc[i][j], b_op[0][j], a_op[0][i]);
+                    const int slot = i * F + j;
+                    read_behind(stage, slot, 1);
+                    if (slot < 32 && slot % 8 == 5) {
+                        if (A_CODES) aim_a(slot / 8);
+                        else aim_b(slot / 8);
+                    }
+                    if (slot >= 32 && slot % 4 == 1) {
+                        decode((slot - 32) / 4);
+                        if (A_CODES) fetch_a((slot - 32) / 4);
+                        else fetch_b((slot - 32) / 4);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        all_reads();
-        barrier();
+            all_reads();
+            barrier();
 #pragma unroll
-        for (int i = 0; i < F; i++)
+            for (int i = 0; i < F; i++)
 #pragma unroll
-            for (int j = 0; j < F; j++) {
-                multiply_accumulated(acc[i][j], b_op[1][j], a_op[1][i]);
-                const int slot = i * F + j;
-                read_behind(stage ^ kPlane, slot, 0);
-                if (slot >= 32 && slot % 4 == 1) {
-                    put_a(stage, (slot - 32) / 4);
-                    if (!A_CODES) fetch_a((slot - 32) / 4);
+                for (int j = 0; j < F; j++) {
+                    multiply_accumulated(acc[i][j], b_op[1][j], a_op[1][i]);
+                    const int slot = i * F + j;
+                    read_behind(stage ^ kPlane, slot, 0);
+                    if (slot < 32 && slot % 8 == 5) {
+                        if (A_CODES) aim_b(slot / 8);
+                        else aim_a(slot / 8);
+                    }
+                    if (slot == 31) step++;
+                    if (slot >= 32 && slot % 4 == 1) {
+                        put_a(stage, (slot - 32) / 4);
+                        if (!A_CODES) fetch_a((slot - 32) / 4);
+                    }
+                    if (slot >= 32 && slot % 4 == 3) {
+                        put_b(stage, (slot - 32) / 4);
+                        if (A_CODES) fetch_b((slot - 32) / 4);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (slot >= 32 && slot % 4 == 3) {
-                    put_b(stage, (slot - 32) / 4);
-                    if (A_CODES) fetch_b((slot - 32) / 4);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            stage ^= kPlane;
+        } while (--more);
+        go_on(run);
+        left -= run;
+        if (left) continue;
+        if constexpr (GATED) break;
+        sums_are_there();
+        done(now, acc);
+        u += gridDim.x;
+        if (u >= units) break;
+        now = unit_of(u);
+        left = now.steps();
+        no_sums(acc);
     }
     all_reads();
-    sums_are_there();
+    if constexpr (GATED) {
+        sums_are_there();
+        done(now, acc);
+    }
 }
 
-// steps of the tile's part
-__device__ inline void wide_steps(const wide_args &t, int part, int &first, int &last)
+// Unit u of `tiles` tiles, in each of the outputs' parts one after the other.
+template <bool GATED>
+__device__ inline wide_unit wide_unit_of(const wide_args &t, int u)
 {
-    const int steps = (int)((t.depth + kWideStep - 1) / kWideStep) * t.terms;
-    first = part * t.steps_a_part;
-    last = min(first + t.steps_a_part, steps) - 1;
+    const int tiles = t.tiles_i * t.tiles_j, of = u / tiles, steps = (int)((t.depth + kWideStep - 1) / kWideStep) * t.terms;
+    int ti, tj;
+    tile_of(t.tiles_i, t.tiles_j, chiplet_order(u % tiles, tiles), ti, tj);
+    const int part = of % t.parts, first = part * t.steps_a_part;
+    return {(int64_t)ti * kWideTile, (int64_t)tj * (GATED ? kWideTile / 2 : kWideTile), of / t.parts, part, first, min(first + t.steps_a_part, steps) - 1};
 }
 
 }  // namespace pvq_fp8_dev
