@@ -39,19 +39,21 @@ struct fp8_matrix {
     int64_t ld = 0;
 };
 
-// Into how many parts the sums of `tiles` tiles of `steps` steps are split: as many as take least, with a workgroup to a unit, 6 us around its steps,
-// and the parts' sums (values of them) written, and read again by a kernel that adds them.
-constexpr double kByteStepUs = 1.4, kWideStepUs = 1.2;       // a step of a 256 x 256 tile: 128 of the sum on the 8-bit, 64 on the bfloat16 instruction
-inline int fp8_parts(int64_t tiles, int64_t steps, double step_us, int64_t values)
+// Into how many parts the sums of `tiles` tiles of `steps` steps are split: as many as take least (us), with a workgroup to a compute unit, a launch, 3 us
+// around each tile's steps, and the parts' sums (values of them) written, and read again by a kernel that adds them.
+constexpr double kByteStepUs = 1.4;                    // a step of a 256 x 256 tile: 128 of the sum on the 8-bit instruction
+constexpr double kWideStepUs = 1.45, kLowStepUs = 0.9;  // 64 of the sum on the bfloat16 instruction; of a tile of 128 x 256
+inline int fp8_parts(int64_t tiles, int64_t steps, double step_us, int64_t values, double *takes = nullptr)
 {
     int best = 1;
     double least = 0.0;
     for (int parts = 1; parts <= 32 && (parts == 1 || steps >= 2 * parts); parts++) {
         const double rounds = (double)((tiles * parts + 255) / 256);
-        double us = rounds * ((double)((steps + parts - 1) / parts) * step_us + 6.0);
+        double us = 5.0 + rounds * ((double)((steps + parts - 1) / parts) * step_us + 3.0);
         if (parts > 1) us += 4.0 + 8.0 * parts * (double)values / 4e6;
         if (parts == 1 || us < least) { best = parts; least = us; }
     }
+    if (takes) *takes = least;
     return best;
 }
 

@@ -5,44 +5,33 @@ using namespace pvq_fp8_dev;
 
 namespace {
 
-template <int KIND>
+template <int KIND, int FI>
 __global__ __launch_bounds__(256) void grad_kernel(wide_args t)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    wide_sums<KIND, false>(t, lds, t.units, [&](int u) { return wide_unit_of<false>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[8][8]) {
+    wide_sums<KIND, false, FI>(t, lds, t.units, [&](int u) { return wide_unit_of<false, FI>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[FI][8]) {
         const wide_args &t = argument<wide_args>();
         const fp8_matrix out = t.parts > 1 ? part_of(t.work, u.out_of * t.parts + u.part, t.rows, t.cols) : u.out_of ? t.out[1] : t.out[0];
         store_sums(out, t.rows, t.cols, acc, u.i0, u.j0);
     });
 }
 
-// the parts of the sum of an output's tiles
-int parts_of(int64_t rows, int64_t cols, int64_t depth, int terms, int outputs)
-{
-    const int64_t tiles = ((rows + kWideTile - 1) / kWideTile) * ((cols + kWideTile - 1) / kWideTile) * outputs;
-    return fp8_parts(tiles, (depth + kWideStep - 1) / kWideStep * terms, kWideStepUs, rows * cols * outputs);
-}
-
 size_t work_of(int64_t rows, int64_t cols, int64_t depth, int terms, int outputs)
 {
-    const int parts = parts_of(rows, cols, depth, terms, outputs);
+    const int parts = wide_plan(rows, cols, depth, terms, outputs).parts;
     return parts > 1 ? (size_t)parts * outputs * rows * cols * 4 : 0;
 }
 
 template <int KIND>
 hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t s)
 {
-    const auto kernel = &grad_kernel<KIND>;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kWideLds);
-    if (e != hipSuccess) return e;
     for (int i = 0; i < g.pairs; i++) { t.dy[i] = g.dy[i]; t.b[i] = g.b[i]; }
     for (int i = 0; i < outputs; i++) t.out[i] = g.out[i];
-    t.tiles_i = (int)((t.rows + kWideTile - 1) / kWideTile);
-    t.tiles_j = (int)((t.cols + kWideTile - 1) / kWideTile);
     t.work = g.work;
-    t.parts = parts_of(t.rows, t.cols, t.depth, t.terms, outputs);
-    t.steps_a_part = (int)(((t.depth + kWideStep - 1) / kWideStep * t.terms + t.parts - 1) / t.parts);
-    t.units = t.tiles_i * t.tiles_j * outputs * t.parts;
+    const wide_tiles plan = t.use(outputs);
+    const auto kernel = plan.low ? &grad_kernel<KIND, 4> : &grad_kernel<KIND, 8>;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kWideLds);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(t.units, 256)), dim3(256), kWideLds, s, t);
     e = hipGetLastError();
     for (int i = 0; i < outputs && t.parts > 1 && e == hipSuccess; i++)

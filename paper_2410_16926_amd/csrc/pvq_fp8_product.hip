@@ -261,13 +261,15 @@ __global__ __launch_bounds__(256) void tile_kernel(tile_args t, tile_out out)
 }
 
 // the same on the bfloat16 instruction
-template <bool GATED>
+template <bool GATED, int FI>
 __global__ __launch_bounds__(256) void wide_tile_kernel(wide_args t, tile_out out)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    wide_sums<WIDE_PRODUCT, GATED>(t, lds, t.units, [&](int u) { return wide_unit_of<GATED>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[8][8]) {
+    wide_sums<WIDE_PRODUCT, GATED, FI>(t, lds, t.units, [&](int u) { return wide_unit_of<GATED, FI>(argument<wide_args>(), u); }, [&](const wide_unit &u, const f32x4 (&acc)[FI][8]) {
         const wide_args &t = argument<wide_args>();
-        store_tile<GATED>(argument<tile_out>(sizeof(wide_args)), t.rows, t.cols, lds, acc, u.i0, u.j0, u.part);
+        const tile_out &out = argument<tile_out>(sizeof(wide_args));
+        if constexpr (GATED) store_tile<GATED>(out, t.rows, t.cols, lds, acc, u.i0, u.j0, u.part);
+        else store_sums(out.parts > 1 ? part_of(out.work, u.part, t.rows, t.cols) : out.y, t.rows, t.cols, acc, u.i0, u.j0);
     });
 }
 
@@ -276,8 +278,8 @@ int64_t tiles_of(int64_t m, int64_t n, bool gated) { return ((m + 255) / 256) * 
 int parts_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide)
 {
     const int64_t values = m * n * (gated ? 2 : 1), tiles = tiles_of(m, n, gated);
-    // (8-bit: parts of whole runs of four blocks, the words of their exponents)
-    return wide ? fp8_parts(tiles, (k + kWideStep - 1) / kWideStep, kWideStepUs, values) : fp8_parts(tiles, (k + 4 * kFp8Block - 1) / (4 * kFp8Block), 4 * kByteStepUs, values);
+    if (!wide) return fp8_parts(tiles, (k + 4 * kFp8Block - 1) / (4 * kFp8Block), 4 * kByteStepUs, values);       // (parts of whole runs of four blocks, the words of their exponents)
+    return gated ? fp8_parts(tiles, (k + kWideStep - 1) / kWideStep, kWideStepUs, values) : wide_plan(m, n, k, 1, 1).parts;
 }
 
 size_t work_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide)
@@ -293,22 +295,33 @@ hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_bloc
     out.parts = k ? parts_of(m, n, k, GATED, wide) : 1;
     const dim3 grid((unsigned)tiles_of(m, n, GATED), (unsigned)out.parts);
     constexpr int kLds = 2 * 2 * 256 * (kFp8Block + 4);
-    const void *kernel = wide ? (const void *)&wide_tile_kernel<GATED> : (const void *)&tile_kernel<GATED>;
-    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, wide ? kWideLds : kLds);
-    if (e != hipSuccess) return e;
-    if (wide) {
-        wide_args t{};
-        t.a = a; t.b[0] = b; t.b[1] = up;
-        t.rows = m; t.cols = n; t.depth = k; t.terms = 1; t.parts = out.parts;
-        t.tiles_i = (int)((m + 255) / 256); t.tiles_j = (int)(grid.x / t.tiles_i);
-        t.steps_a_part = (int)(((k + kWideStep - 1) / kWideStep + t.parts - 1) / t.parts);
-        t.units = (int)(grid.x * grid.y);
-        hipLaunchKernelGGL(wide_tile_kernel<GATED>, dim3((unsigned)(GATED ? t.units : std::min(t.units, 256))), dim3(256), kWideLds, s, t, out);
-    } else {
+    auto allow = [](auto kernel, int bytes) { return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+    if (!wide) {
+        const hipError_t e = allow(&tile_kernel<GATED>, kLds);
+        if (e != hipSuccess) return e;
         tile_args t{a, b, up, n, (int)((m + 255) / 256), 0, 0};
         t.tiles_n = (int)(grid.x / t.tiles_m);
         t.blocks_a_part = (int)(((a.blocks() + 3) / 4 + out.parts - 1) / out.parts * 4);
         hipLaunchKernelGGL(tile_kernel<GATED>, grid, dim3(256), kLds, s, t, out);
+        return hipGetLastError();
+    }
+    wide_args t{};
+    t.a = a; t.b[0] = b; t.b[1] = up;
+    t.rows = m; t.cols = n; t.depth = k; t.terms = 1;
+    if constexpr (GATED) {
+        const hipError_t e = allow(&wide_tile_kernel<true, 8>, kWideLds);
+        if (e != hipSuccess) return e;
+        t.parts = out.parts;
+        t.tiles_i = (int)((m + 255) / 256); t.tiles_j = (int)(grid.x / t.tiles_i);
+        t.steps_a_part = (int)(((k + kWideStep - 1) / kWideStep + t.parts - 1) / t.parts);
+        t.units = (int)(grid.x * grid.y);
+        hipLaunchKernelGGL((wide_tile_kernel<true, 8>), dim3((unsigned)t.units), dim3(256), kWideLds, s, t, out);
+    } else {
+        const auto kernel = t.use(1).low ? &wide_tile_kernel<false, 4> : &wide_tile_kernel<false, 8>;
+        const hipError_t e = allow(kernel, kWideLds);
+        if (e != hipSuccess) return e;
+        out.parts = t.parts;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(t.units, 256)), dim3(256), kWideLds, s, t, out);
     }
     return hipGetLastError();
 }

@@ -109,12 +109,13 @@ __device__ __forceinline__ const T &argument(int offset = 0)
 }
 
 // All sums zero, where they are.
-__device__ __forceinline__ void no_sums(f32x4 (&acc)[8][8])
+template <int FI>
+__device__ __forceinline__ void no_sums(f32x4 (&acc)[FI][8])
 {
     u32x4 zero{0, 0, 0, 0};
     asm volatile("s_nop 7" : "+v"(zero));                // (written, and some instructions before the first below)
 #pragma unroll
-    for (int i = 0; i < 8; i++)
+    for (int i = 0; i < FI; i++)
 #pragma unroll
         for (int j = 0; j < 8; j++) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %1, 0" : "+a"(acc[i][j]) : "v"(zero));
 }
@@ -148,21 +149,22 @@ __device__ __forceinline__ void store_rows(uint8_t *lds, const f32x4 (&acc)[8][8
     }
 }
 
-// A tile's sums to a matrix, the tile's first at row0, col0, from where they are: LDS may hold the next tile's operands by now.  Four waves of 128 x 128;
+// A tile's sums to a matrix, the tile's first at row0, col0, from where they are: LDS may hold the next tile's operands by now.  Four waves of 16 FI x 128;
 // a lane has four neighbouring columns of one row of a fragment.  float32 is stored so, 16 rows of 64 bytes at a time.  Of 16-bit types two fragments'
 // halves and quarters change places, after which a lane has eight neighbouring columns: 64 bytes of a row again.  (Every sum is read at one place,
 // whatever the type: of reads in several branches the compiler moves some up, to where the sums need not be there yet.)
-__device__ __forceinline__ void store_sums(const fp8_matrix &y, int64_t rows, int64_t cols, const f32x4 (&acc)[8][8], int64_t row0, int64_t col0)
+template <int FI>
+__device__ __forceinline__ void store_sums(const fp8_matrix &y, int64_t rows, int64_t cols, const f32x4 (&acc)[FI][8], int64_t row0, int64_t col0)
 {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
-    row0 += wave / 2 * 128;
+    row0 += wave / 2 * 16 * FI;
     col0 += wave % 2 * 128;
-    const bool inside = row0 + 128 <= rows && col0 + 128 <= cols, f32 = y.dtype == PVQ_F32, bf16 = y.dtype == PVQ_BF16;
+    const bool inside = row0 + 16 * FI <= rows && col0 + 128 <= cols, f32 = y.dtype == PVQ_F32, bf16 = y.dtype == PVQ_BF16;
     const int bytes = f32 ? 4 : 2;
     const int64_t row = row0 + r16, col = col0 + quarter * (f32 ? 4 : 8);
     uint8_t *to = reinterpret_cast<uint8_t *>(y.data) + (row * y.ld + col) * bytes;
 #pragma unroll
-    for (int i = 0; i < 8; i++, to += 16 * y.ld * bytes) {
+    for (int i = 0; i < FI; i++, to += 16 * y.ld * bytes) {
         const bool there = row + 16 * i < rows;
         const int64_t left = there ? cols - col : 0;
         __builtin_amdgcn_sched_barrier(0);

@@ -15,6 +15,21 @@ enum wide_kind {
     WIDE_WEIGHT_GRAD,    // A(i, r) = dy[r][i], B(r, j) = b[r][j]
 };
 
+// Tiles of 256 x 256, or low ones of 128 x 256 where these take less: a step of them is 64 matrix instructions less but the same codes to decode.
+struct wide_tiles {
+    bool low;
+    int parts;
+    int rows() const { return low ? 128 : 256; }
+};
+inline wide_tiles wide_plan(int64_t rows, int64_t cols, int64_t depth, int terms, int outputs)
+{
+    const int64_t across = (cols + kWideTile - 1) / kWideTile * outputs, steps = (depth + kWideStep - 1) / kWideStep * terms, values = rows * cols * outputs;
+    double us, low_us;
+    const int parts = fp8_parts((rows + 255) / 256 * across, steps, kWideStepUs, values, &us), low_parts = fp8_parts((rows + 127) / 128 * across, steps, kLowStepUs, values, &low_us);
+    const bool low = low_us < us;
+    return {low, low ? low_parts : parts};
+}
+
 struct wide_args {
     fp8_bf16 dy[2];                  // of the terms, or of the outputs; rows aligned to 16 bytes, for input gradients whole 64s or zeros behind their last value
     fp8_blocks a, b[2];              // b: of the terms or outputs; the gate's and the up weights
@@ -24,6 +39,18 @@ struct wide_args {
     int tiles_i, tiles_j;
     int parts, steps_a_part;         // of a split sum, whose parts go to work
     int units;                       // tiles of all parts of all outputs
+
+    // the tiles that wide_plan takes
+    wide_tiles use(int outputs)
+    {
+        const wide_tiles plan = wide_plan(rows, cols, depth, terms, outputs);
+        parts = plan.parts;
+        tiles_i = (int)((rows + plan.rows() - 1) / plan.rows());
+        tiles_j = (int)((cols + kWideTile - 1) / kWideTile);
+        steps_a_part = (int)(((depth + kWideStep - 1) / kWideStep * terms + parts - 1) / parts);
+        units = tiles_i * tiles_j * outputs * parts;
+        return plan;
+    }
     float *work;
 };
 
@@ -50,26 +77,28 @@ struct wide_unit {
 // A workgroup has units blockIdx.x, blockIdx.x + gridDim.x .. and goes from one to the next without a pause: three steps ahead of the products, its loads
 // are the next unit's when one ends, and between two steps the sums are stored from where they are.  (GATED: one unit, and done may use LDS.)
 // dW of 64 x 16384 x 4096, four tiles of one step to a workgroup, 38 us; with a workgroup to each tile, stored by way of LDS, 50; 576 tokens 85 and 97.
-template <int KIND, bool GATED, typename UNIT, typename DONE>
+template <int KIND, bool GATED, int FI, typename UNIT, typename DONE>
 __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int units, UNIT unit_of, DONE done)
 {
-    constexpr int F = 8, kPlane = kWideTile * kWideStep * 2, kPieces = 8;       // LDS: A's two stages, B's two stages
+    constexpr int F = 8, kPlane = kWideTile * kWideStep * 2, kPieces = 8, kSlots = FI * F;       // LDS: A's two stages, B's two stages
+    static_assert(FI == 8 || (FI == 4 && !GATED), "rows");
     constexpr bool A_ALONG = KIND != WIDE_WEIGHT_GRAD, B_ALONG = KIND == WIDE_PRODUCT, A_CODES = KIND == WIDE_PRODUCT;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int wi = wave / 2, wj = wave % 2, r16 = lane % 16, quarter = lane / 16;
     const int steps_a_term = (int)((t.depth + kWideStep - 1) / kWideStep);
 
     // Strides in bytes (the same for both terms or outputs).  A lane's piece is eight values of a row; an operand whose rows run along the sum has eight
-    // lanes to a row, one whose rows run across it 32, and piece p is 32 or 8 rows behind piece p - 1.
+    // lanes to a row, one whose rows run across it 32 (A of 128 columns 16), and piece p is 32 or 8 (16) rows behind piece p - 1.
     const uint32_t a_row = A_CODES ? (uint32_t)t.a.code_row() : (uint32_t)t.dy[0].ld * 2, b_row = (uint32_t)t.b[0].code_row();
     const uint32_t ae_row = (uint32_t)t.a.exp_row(), be_row = (uint32_t)t.b[0].exp_row();
-    const uint32_t along_row = tid / 8, along_col = tid % 8 * 8, across_row = tid / 32, across_col = tid % 32 * 8;
-    const uint32_t a_at = (A_ALONG ? along_row * a_row + along_col * (A_CODES ? 1 : 2) : across_row * a_row + across_col * 2), a_next = (A_ALONG ? 32 : 8) * a_row;
+    constexpr int kALanes = 4 * FI;        // to a row of A that runs across the sum
+    const uint32_t along_row = tid / 8, along_col = tid % 8 * 8, across_row = tid / 32, across_col = tid % 32 * 8, a_across_row = tid / kALanes, a_across_col = tid % kALanes * 8;
+    const uint32_t a_at = (A_ALONG ? along_row * a_row + along_col * (A_CODES ? 1 : 2) : a_across_row * a_row + a_across_col * 2), a_next = (A_ALONG ? 32 : 256 / kALanes) * a_row;
     const uint32_t b_at = B_ALONG ? along_row * b_row + along_col : across_row * b_row + across_col, b_next = (B_ALONG ? 32 : 8) * b_row;
     const uint32_t be_at = B_ALONG ? along_row * be_row : across_row * be_row + across_col / kFp8Block, be_next = (B_ALONG ? 32 : 8) * be_row;
     const uint32_t ae_at = along_row * ae_row, ae_next = 32 * ae_row;
 
-    u32x4 ra[kPieces];               // (codes: the first two words, and the exponent)
+    u32x4 ra[FI];                    // (codes: the first two words, and the exponent)
     u32x2 rb[kPieces];
     uint32_t re[kPieces];
     bf16x8 decoded[kPieces];         // A's codes, or else B's, for the next half
@@ -168,43 +197,45 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         re[p] = __builtin_amdgcn_raw_buffer_load_b8(up ? ue_from : be_from, be_at, in * be_next, 0);
     };
 
-    // Rows across the sum lie in LDS as in memory, [r][256 columns], in pieces of sixteen columns; the transposing read gives a lane four neighbouring r
+    // Rows across the sum lie in LDS as in memory, [r][256 columns] (or 128), in pieces of sixteen columns; the transposing read gives a lane four neighbouring r
     // of one column.  Piece c of row r lies at place c ^ f(r), f = r % 4 + 4 (r / 8 % 2): the eight rows that 32 lanes read at once lie in different
     // banks.  Rows along the sum: [row][64 r], chunk c (eight r) of row i at place c ^ (i / 2 % 8).
     const uint32_t across_to = across_row * 512 + (((across_col / 16) ^ (across_row & 3)) << 5) + across_col % 16 * 2, across_odd = across_to ^ (4 << 5);
     const uint32_t along_to = along_row * 128 + (((along_col / 8) ^ (along_row / 2 & 7)) << 4);
-    auto place = [&](bool along, int p) { return p * 4096 + (along ? along_to : p & 1 ? across_odd : across_to); };
+    const uint32_t a_across_to = a_across_row * kALanes * 16 + (((a_across_col / 16) ^ (a_across_row & 3) ^ (FI == 4 ? a_across_row / 8 * 4 : 0)) << 5) + a_across_col % 16 * 2;
+    auto place_a = [&](int p) { return p * 4096 + (A_ALONG ? along_to : FI == 8 && p & 1 ? a_across_to ^ (4 << 5) : a_across_to); };
+    auto place_b = [&](int p) { return p * 4096 + (B_ALONG ? along_to : p & 1 ? across_odd : across_to); };
     auto decode = [&](int p) {
         if constexpr (A_CODES) decoded[p] = bf16x8_of_codes(ra[p][0], ra[p][1], scale_of(ra[p][2]));
         else decoded[p] = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
     };
     auto put_a = [&](uint32_t stage, int p) {
-        uint8_t *to = lds + stage + place(A_ALONG, p);
+        uint8_t *to = lds + stage + place_a(p);
         if constexpr (A_CODES) *reinterpret_cast<bf16x8 *>(to) = decoded[p];
         else *reinterpret_cast<u32x4 *>(to) = ra[p];
     };
     auto put_b = [&](uint32_t stage, int p) {
-        bf16x8 *to = reinterpret_cast<bf16x8 *>(lds + stage + 2 * kPlane + place(B_ALONG, p));
+        bf16x8 *to = reinterpret_cast<bf16x8 *>(lds + stage + 2 * kPlane + place_b(p));
         if constexpr (A_CODES) *to = bf16x8_of_codes(rb[p][0], rb[p][1], scale_of(re[p]));
         else *to = decoded[p];
     };
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const uint32_t sub = lane % 16, f = sub / 4 | (quarter & 1) << 2, row_at = (8 * quarter + sub / 4) * 512 + (sub % 4) * 8;
-    auto read_across = [&](uint32_t plane, int column, int h) {       // sixteen columns from 16 * column on
-        const uint8_t *from = lds + plane + h * 32 * 512 + (column / 8) * 256 + (((column % 8) ^ f) << 5) + row_at;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * 512));
+    const uint32_t sub = lane % 16, f = sub / 4 | (quarter & 1) << 2, row_of = 8 * quarter + sub / 4;
+    auto read_across = [&](uint32_t plane, int row_bytes, int column, int h) {       // sixteen columns from 16 * column on
+        const uint8_t *from = lds + plane + h * 32 * row_bytes + (column / 8) * 256 + (((column % 8) ^ f) << 5) + row_of * row_bytes + (sub % 4) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * row_bytes));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     auto read_along = [&](uint32_t plane, int row, int h) {           // sixteen rows from `row` on
         return *reinterpret_cast<const bf16x8 *>(lds + plane + (row + r16) * 128 + (((4 * h + quarter) ^ (r16 >> 1)) << 4));
     };
-    auto read_a = [&](uint32_t stage, int i, int h) { return A_ALONG ? read_along(stage, wi * 128 + i * 16, h) : read_across(stage, wi * 8 + i, h); };
+    auto read_a = [&](uint32_t stage, int i, int h) { return A_ALONG ? read_along(stage, (wi * FI + i) * 16, h) : read_across(stage, kALanes * 16, wi * FI + i, h); };
     auto read_b = [&](uint32_t stage, int j, int h) {
-        return B_ALONG ? read_along(stage + 2 * kPlane, GATED ? (j / 4) * 128 + wj * 64 + (j % 4) * 16 : wj * 128 + j * 16, h) : read_across(stage + 2 * kPlane, wj * 8 + j, h);
+        return B_ALONG ? read_along(stage + 2 * kPlane, GATED ? (j / 4) * 128 + wj * 64 + (j % 4) * 16 : wj * 128 + j * 16, h) : read_across(stage + 2 * kPlane, 512, wj * 8 + j, h);
     };
 
-    f32x4 acc[F][F];
-    bf16x8 a_op[2][F], b_op[2][F];
+    f32x4 acc[FI][F];
+    bf16x8 a_op[2][FI], b_op[2][F];
 
     auto fetch_all = [&] {
 #pragma unroll
@@ -212,31 +243,46 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         step++;
         go_on(1);
 #pragma unroll
-        for (int p = 0; p < kPieces; p++) { fetch_a(p); fetch_b(p); }
+        for (int p = 0; p < kPieces; p++) {
+            if (p < FI) fetch_a(p);
+            fetch_b(p);
+        }
     };
     // the reads of a half's operands behind its predecessor's first 32 instructions
     auto read_behind = [&](uint32_t stage, int slot, int h) {
         if (slot % 2 == 0 && slot / 2 < F) b_op[h][slot / 2] = read_b(stage, slot / 2, h);
-        if (slot % 2 == 0 && slot / 2 >= F && slot / 2 < 2 * F) a_op[h][slot / 2 - F] = read_a(stage, slot / 2 - F, h);
+        if (slot % 2 == 0 && slot / 2 >= F && slot / 2 < F + FI) a_op[h][slot / 2 - F] = read_a(stage, slot / 2 - F, h);
     };
+    // which piece's turn it is behind an instruction: the first one's behind `from`, the next `every` on
+    auto piece_of = [](int slot, int from, int every, int pieces) { return slot >= from && (slot - from) % every == 0 && (slot - from) / every < pieces ? (slot - from) / every : -1; };
     wide_unit now = ahead;
     int u = blockIdx.x, left = now.steps();
     start();
     {
         // (the second step's on its way while the first is waited for)
-        u32x4 a[2][kPieces];
+        u32x4 a[2][FI];
         u32x2 b[2][kPieces];
         uint32_t e[2][kPieces];
 #pragma unroll
         for (int s = 0; s < 2; s++) {
             fetch_all();
 #pragma unroll
-            for (int p = 0; p < kPieces; p++) { a[s][p] = ra[p]; b[s][p] = rb[p]; e[s][p] = re[p]; }
+            for (int p = 0; p < FI; p++) a[s][p] = ra[p];
+#pragma unroll
+            for (int p = 0; p < kPieces; p++) { b[s][p] = rb[p]; e[s][p] = re[p]; }
         }
 #pragma unroll
         for (int s = 0; s < 2; s++) {
 #pragma unroll
-            for (int p = 0; p < kPieces; p++) { ra[p] = a[s][p]; rb[p] = b[s][p]; re[p] = e[s][p]; decode(p); put_a(s * kPlane, p); put_b(s * kPlane, p); }
+            for (int p = 0; p < FI; p++) ra[p] = a[s][p];
+#pragma unroll
+            for (int p = 0; p < kPieces; p++) { rb[p] = b[s][p]; re[p] = e[s][p]; }
+#pragma unroll
+            for (int p = 0; p < kPieces; p++) {
+                if (!A_CODES || p < FI) decode(p);
+                if (p < FI) put_a(s * kPlane, p);
+                put_b(s * kPlane, p);
+            }
         }
     }
     fetch_all();
@@ -245,7 +291,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
 #pragma unroll
     for (int j = 0; j < F; j++) b_op[0][j] = read_b(0, j, 0);
 #pragma unroll
-    for (int i = 0; i < F; i++) a_op[0][i] = read_a(0, i, 0);
+    for (int i = 0; i < FI; i++) a_op[0][i] = read_a(0, i, 0);
     no_sums(acc);
     // (stages by the offset of their planes, 0 or kPlane: one body for all steps, whose sums stay where they are)
     // In runs without a condition, until either the products or the loads come to an end of theirs.
@@ -255,44 +301,48 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         int more = run;
         do {
 #pragma unroll
-            for (int i = 0; i < F; i++)
+            for (int i = 0; i < FI; i++)
 #pragma unroll
                 for (int j = 0; j < F; j++) {
                     multiply_accumulated(acc[i][j], b_op[0][j], a_op[0][i]);
                     const int slot = i * F + j;
                     read_behind(stage, slot, 1);
-                    if (slot < 32 && slot % 8 == 5) {
-                        if (A_CODES) aim_a(slot / 8);
-                        else aim_b(slot / 8);
+                    const int aim = piece_of(slot, FI == 8 ? 5 : 1, FI == 8 ? 8 : 4, GATED ? 4 : 2);
+                    if (aim >= 0) {
+                        if (A_CODES) aim_a(aim);
+                        else aim_b(aim);
                     }
-                    if (slot >= 32 && slot % 4 == 1) {
-                        decode((slot - 32) / 4);
-                        if (A_CODES) fetch_a((slot - 32) / 4);
-                        else fetch_b((slot - 32) / 4);
+                    const int piece = piece_of(slot, FI == 8 ? 33 : 17, FI == 8 ? 4 : 2, A_CODES ? FI : kPieces);
+                    if (piece >= 0) {
+                        decode(piece);
+                        if (A_CODES) fetch_a(piece);
+                        else fetch_b(piece);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             all_reads();
             barrier();
 #pragma unroll
-            for (int i = 0; i < F; i++)
+            for (int i = 0; i < FI; i++)
 #pragma unroll
                 for (int j = 0; j < F; j++) {
                     multiply_accumulated(acc[i][j], b_op[1][j], a_op[1][i]);
                     const int slot = i * F + j;
                     read_behind(stage ^ kPlane, slot, 0);
-                    if (slot < 32 && slot % 8 == 5) {
-                        if (A_CODES) aim_b(slot / 8);
-                        else aim_a(slot / 8);
+                    const int aim = piece_of(slot, FI == 8 ? 5 : 1, FI == 8 ? 8 : 4, GATED ? 4 : 2);        // (before the fetches below)
+                    if (aim >= 0) {
+                        if (A_CODES) aim_b(aim);
+                        else aim_a(aim);
                     }
                     if (slot == 31) step++;
-                    if (slot >= 32 && slot % 4 == 1) {
-                        put_a(stage, (slot - 32) / 4);
-                        if (!A_CODES) fetch_a((slot - 32) / 4);
+                    const int piece = piece_of(slot, FI == 8 ? 33 : 25, FI == 8 ? 4 : 2, FI), piece_b = piece_of(slot, FI == 8 ? 35 : 9, FI == 8 ? 4 : 2, kPieces);
+                    if (piece >= 0) {
+                        put_a(stage, piece);
+                        if (!A_CODES) fetch_a(piece);
                     }
-                    if (slot >= 32 && slot % 4 == 3) {
-                        put_b(stage, (slot - 32) / 4);
-                        if (A_CODES) fetch_b((slot - 32) / 4);
+                    if (piece_b >= 0) {
+                        put_b(stage, piece_b);
+                        if (A_CODES) fetch_b(piece_b);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -318,14 +368,14 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
 }
 
 // Unit u of `tiles` tiles, in each of the outputs' parts one after the other.
-template <bool GATED>
+template <bool GATED, int FI>
 __device__ inline wide_unit wide_unit_of(const wide_args &t, int u)
 {
     const int tiles = t.tiles_i * t.tiles_j, of = u / tiles, steps = (int)((t.depth + kWideStep - 1) / kWideStep) * t.terms;
     int ti, tj;
     tile_of(t.tiles_i, t.tiles_j, chiplet_order(u % tiles, tiles), ti, tj);
     const int part = of % t.parts, first = part * t.steps_a_part;
-    return {(int64_t)ti * kWideTile, (int64_t)tj * (GATED ? kWideTile / 2 : kWideTile), of / t.parts, part, first, min(first + t.steps_a_part, steps) - 1};
+    return {(int64_t)ti * 32 * FI, (int64_t)tj * (GATED ? kWideTile / 2 : kWideTile), of / t.parts, part, first, min(first + t.steps_a_part, steps) - 1};
 }
 
 }  // namespace pvq_fp8_dev
