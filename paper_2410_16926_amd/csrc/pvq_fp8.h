@@ -42,7 +42,7 @@ struct fp8_matrix {
 // Into how many parts the sums of `tiles` tiles of `steps` steps are split: as many as take least (us), with a workgroup to a compute unit, a launch, 3 us
 // around each tile's steps, and the parts' sums (values of them) written, and read again by a kernel that adds them.
 constexpr double kByteStepUs = 1.4;                    // a step of a 256 x 256 tile: 128 of the sum on the 8-bit instruction
-constexpr double kWideStepUs = 1.45, kLowStepUs = 0.9;  // 64 of the sum on the bfloat16 instruction; of a tile of 128 x 256
+constexpr double kWideStepUs = 1.75, kLowStepUs = 1.2;  // 64 of the sum on the bfloat16 instruction; of a tile of 128 x 256 (short runs, at full clocks: 1.45 and 0.9)
 inline int fp8_parts(int64_t tiles, int64_t steps, double step_us, int64_t values, double *takes = nullptr)
 {
     int best = 1;
