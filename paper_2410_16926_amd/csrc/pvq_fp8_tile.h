@@ -12,10 +12,6 @@ __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t l
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
-__device__ inline void load_words_to_lds(const void *base, uint32_t offset, uint32_t lds)     // 4 bytes a lane
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
-}
 // The same from a buffer of `bytes` bytes (below 4 GiB), base, size and `uniform` in scalar registers: nothing is fetched from behind its end.
 typedef __attribute__((ext_vector_type(4))) uint32_t buffer_t;
 __device__ inline buffer_t make_buffer(const void *base, int64_t bytes)
@@ -24,14 +20,17 @@ __device__ inline buffer_t make_buffer(const void *base, int64_t bytes)
     return buffer_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFFu,
                     (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes), 0x00020000u};
 }
+// (these have `lds` for an operand, not in their name: no register of theirs is written)
+#define PVQ_BUFFER_TO_LDS(width) "s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_" width " %1, %2, %3 offen lds"
 __device__ inline void load_to_lds(buffer_t from, uint32_t offset, uint32_t uniform, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
+    asm volatile(PVQ_BUFFER_TO_LDS("dwordx4") : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
 }
-__device__ inline void load_words_to_lds(buffer_t from, uint32_t offset, uint32_t uniform, uint32_t lds)
+__device__ inline void load_words_to_lds(buffer_t from, uint32_t offset, uint32_t uniform, uint32_t lds)     // 4 bytes a lane
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
+    asm volatile(PVQ_BUFFER_TO_LDS("dword") : : "s"(lds), "v"(offset), "s"(from), "s"(uniform) : "memory", "m0");
 }
+#undef PVQ_BUFFER_TO_LDS
 __device__ inline void all_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 // all but the last N
