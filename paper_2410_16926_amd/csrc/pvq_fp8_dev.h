@@ -119,7 +119,12 @@ __device__ inline uint32_t block_exponent(const float (&v)[8])
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) top = max(top, finite_bits(v[i]));
+    for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    if (__builtin_amdgcn_ballot_w64(top >= 0x7F800000u)) {             // (seldom: infinities or NaN in the wave)
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = max(top, finite_bits(v[i]));
+    }
     return exponent_of(block_max(top));
 }
 
@@ -178,11 +183,13 @@ __device__ inline void store_gated8(const gated_out &t, int64_t row, int64_t n, 
 {
     const int64_t count = n - col, code_row = (n + kFp8Block - 1) / kFp8Block * kFp8Block, exp_row = (code_row / kFp8Block + 3) / 4 * 4;
     float h[8];
+    if (count < 8) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        if (i >= count) g[i] = u[i] = 0.0f;
-        h[i] = act_value<ACT>(g[i]) * u[i];
+        for (int i = 0; i < 8; i++)
+            if (i >= count) g[i] = u[i] = 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < 8; i++) h[i] = act_value<ACT>(g[i]) * u[i];
     if (t.h.data && row_there && count > 0) store_values(t.h, row, col, count, h);
     auto to_blocks = [&](uint8_t *codes, uint8_t *exps, const float (&v)[8]) {
         if (!codes) return;
