@@ -347,8 +347,8 @@ int pvq_fp8_decode(const uint8_t *codes, const uint8_t *exponents, int64_t rows,
  * Y = A B^T, A [m][k] and B [n][k] in blocks, Y [m][ldy] of out_dtype: tokens times weights, any number of tokens.
  * Sums are float32.  To PVQ_F32 they are formed of the decoded values by the bfloat16 matrix instructions; to PVQ_BF16 and PVQ_F16
  * by the 8-bit ones, which align the products of a group of eight to the largest among them and drop what lies 14 bits below
- * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 32) take the
- * bfloat16 instructions for every type.  The order of the sums depends on the shape alone.
+ * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 32) and small
+ * products take the bfloat16 instructions for every type.  The order of the sums depends on the shape alone.
  *   work   device, 16-byte aligned scratch of pvq_fp8_product_work_bytes bytes (may be NULL where that is 0); calls that
  *          may overlap in time need one each
  * k == 0 gives zeros.
@@ -363,8 +363,8 @@ int pvq_fp8_product(const uint8_t *a_codes, const uint8_t *a_exponents, int64_t 
  *   pvq_fp8_input_grad    dX = dY W    [m][lddx] of out_dtype
  *   pvq_fp8_weight_grad   dW = dY^T X  [n][lddw] of out_dtype
  * On the bfloat16 matrix instructions, the blocks decoded exactly, sums in float32 and one rounding to out_dtype.
- * work as for pvq_fp8_product; its size depends on dY and lddy by their alignment alone (rows that do not start at 16 bytes are copied
- * there first, for dX also those whose n is no multiple of 64).
+ * work as for pvq_fp8_product; its size depends on dY and lddy by their alignment alone (for large products rows that do not start at
+ * 16 bytes are copied there first, for dX also those whose n is no multiple of 64).
  */
 int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const uint8_t *w_codes, const uint8_t *w_exponents, int64_t n,

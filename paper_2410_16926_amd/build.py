@@ -20,7 +20,7 @@ SOURCES = ["pvq_host.cpp", "pvq_fast8_tables.cpp", "pvq_kernels.hip", "pvq_fast8
            "pvq_exact_check.hip", "pvq_fp8_host.cpp", "pvq_fp8_blocks.hip", "pvq_fp8_product.hip", "pvq_fp8_rows.hip", "pvq_fp8_grad.hip"]
 
 HEADERS = ["pvq_internal.h", "pvq_fast8.h", "pvq_hadamard_dev.h", "pvq_quantize_dev.h", "pvq_diagnostics.h", "pvq_small_table.h",
-           "pvq_walk.h", "pvq_exact_dev.h", "pvq_fp8.h", "pvq_fp8_dev.h", "pvq_fp8_tile.h", "pvq_fp8_wide.h"]
+           "pvq_walk.h", "pvq_exact_dev.h", "pvq_fp8.h", "pvq_fp8_dev.h", "pvq_fp8_tile.h", "pvq_fp8_wide.h", "pvq_fp8_small.h"]
 
 # -ffp-contract=off: the encoder's float32 results are part of the format (no fused multiply-adds
 # unless written as fmaf); correctly rounded float32 division and square root likewise.

@@ -57,6 +57,23 @@ inline int fp8_parts(int64_t tiles, int64_t steps, double step_us, int64_t value
     return best;
 }
 
+// The same for tiles of 64 x 64 (GATED: 32 hidden units), a step 64 of the sum.  Several workgroups share a unit and fill it between each other's waits.
+// join: the parts' sums go to work and are added (or taken to blocks) by a kernel of its own, however few they are.
+constexpr double kSmallStepUs = 0.3, kSmallBusyUs = 0.28;      // a step of a workgroup alone on its unit, and a unit's time for it where there are several (dX; the others 0.21)
+inline int fp8_small_parts(int64_t tiles, int64_t steps, int64_t values, bool join, double *takes)
+{
+    int best = 1;
+    double least = 0.0;
+    for (int parts = 1; parts <= 16 && (parts == 1 || steps >= 8 * parts); parts++) {
+        const double a_part = (double)((steps + parts - 1) / parts), a_unit = (double)((tiles * parts + 255) / 256);
+        double us = 6.0 + a_part * std::max(kSmallStepUs, a_unit * kSmallBusyUs) + (double)(tiles * parts) * 0.003;
+        if (parts > 1 || join) us += 4.0 + 8.0 * parts * (double)values / 4e6;
+        if (parts == 1 || us < least) { best = parts; least = us; }
+    }
+    *takes = least;
+    return best;
+}
+
 // Y = A B^T.  work: float32 sums of the parts of a split (fp8_product_work), unused without one.
 struct fp8_product_args {
     fp8_blocks a, b;
@@ -74,8 +91,8 @@ struct fp8_gated_args {
     uint8_t *hc, *he, *gc, *ge, *uc, *ue;
     float *work;
 };
-// wide: sums on the bfloat16 instruction (float32 results, kept products)
-size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide);
+// wide: sums on the bfloat16 instruction (float32 results, kept products); to_blocks: H in blocks, or G and U kept
+size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide, bool to_blocks);
 hipError_t fp8_launch_gated(const fp8_gated_args &a, hipStream_t s);
 // ... of the parts of G and U, [parts][2][rows][cols]
 hipError_t fp8_launch_gated_join(const float *work, int parts, const fp8_gated_args &a, hipStream_t s);
@@ -100,6 +117,9 @@ struct fp8_grad_args {
     fp8_matrix out[2];
     float *work;
 };
+// whether a single gradient's dY is taken with rows that start and end anywhere
+bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k);
+bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k);
 size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
 size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
 hipError_t fp8_launch_input_grad(const fp8_grad_args &a, hipStream_t s);

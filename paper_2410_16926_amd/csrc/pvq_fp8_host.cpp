@@ -51,13 +51,17 @@ int first_of(std::initializer_list<int> codes)
 // the row stride of a workspace's bfloat16 matrices, in values
 int64_t slope_row(int64_t n) { return (n + 63) / 64 * 64; }
 
-// Whether the gradient kernels can take dY as it is: rows aligned to 16 bytes, a tile's within 32-bit offsets, and where they run along
+// Whether the gradient kernels of large tiles can take dY as it is: rows aligned to 16 bytes, a tile's within 32-bit offsets, and where they run along
 // the sum (dX) in whole steps of it.  Otherwise it is copied first, with zeros behind the rows.
 bool whole_rows(const void *dY, int64_t ld, int64_t n, bool along) { return aligned(dY, 16) && ld % 8 == 0 && ld <= kMostCols && (!along || n % 64 == 0); }
 
 size_t up16(size_t v) { return (v + 15) / 16 * 16; }
 
-size_t copy_bytes(const void *dY, int64_t ld, int64_t m, int64_t n, bool along) { return whole_rows(dY, ld, n, along) ? 0 : up16((size_t)m * slope_row(n) * 2); }
+size_t copy_bytes(const void *dY, int64_t ld, int64_t m, int64_t n, int64_t k, bool along)
+{
+    const bool as_it_is = along ? fp8_input_grad_as_it_is(m, n, k) : fp8_weight_grad_as_it_is(m, n, k);
+    return as_it_is || whole_rows(dY, ld, n, along) ? 0 : up16((size_t)m * slope_row(n) * 2);
+}
 
 // a gradient's dY, copied to the front of its workspace where it has to be; the split's sums behind it
 hipError_t take_dy(fp8_grad_args &a, void *work, size_t copy, hipStream_t s)
@@ -130,7 +134,7 @@ extern "C" int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, true) + fp8_input_grad_work(m, n, k, 1) : 0;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, true) + fp8_input_grad_work(m, n, k, 1) : 0;
     return PVQ_OK;
 }
 
@@ -151,7 +155,7 @@ extern "C" int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const
         return rc;
     const hipStream_t s = (hipStream_t)stream;
     if (n == 0) return status_of(fp8_launch_join(nullptr, 0, m, k, a.out[0], s));
-    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n, true), s);
+    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n, k, true), s);
     return status_of(e == hipSuccess ? fp8_launch_input_grad(a, s) : e);
 }
 
@@ -159,7 +163,7 @@ extern "C" int pvq_fp8_weight_grad_work_bytes(const void *dY, int64_t lddy, int6
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, false) + fp8_weight_grad_work(m, n, k, 1) : 0;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, false) + fp8_weight_grad_work(m, n, k, 1) : 0;
     return PVQ_OK;
 }
 
@@ -180,7 +184,7 @@ extern "C" int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int6
         return rc;
     const hipStream_t s = (hipStream_t)stream;
     if (m == 0) return status_of(fp8_launch_join(nullptr, 0, n, k, a.out[0], s));
-    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n, false), s);
+    const hipError_t e = take_dy(a, work, copy_bytes(dY, lddy, m, n, k, false), s);
     return status_of(e == hipSuccess ? fp8_launch_weight_grad(a, s) : e);
 }
 
@@ -188,7 +192,7 @@ extern "C" int pvq_fp8_gated_work_bytes(int64_t m, int64_t n, int64_t k, int out
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!known(out_dtype) || !bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k && (to_blocks || !fp8_rows_pay(m)) ? std::max(fp8_gated_work(m, n, k, false), fp8_gated_work(m, n, k, true)) : 0;
+    *bytes = m && n && k && (to_blocks || !fp8_rows_pay(m)) ? std::max(fp8_gated_work(m, n, k, false, to_blocks), fp8_gated_work(m, n, k, true, to_blocks)) : 0;
     return PVQ_OK;
 }
 

@@ -1,5 +1,5 @@
 // Products of 8-bit block matrices in tiles: Y = A B^T, and the gated block H = act(X Wg^T) * (X Wu^T).
-#include "pvq_fp8_wide.h"
+#include "pvq_fp8_small.h"
 
 #include <type_traits>
 
@@ -32,7 +32,7 @@ struct tile_args {
 struct tile_out {
     fp8_matrix y;                // of a product
     gated_out gated;
-    int parts;                   // of a split, whose sums go to work: [part][rows][n], GATED [part][G, U][rows][n]
+    int parts;                   // whose sums go to work, [part][rows][n], GATED [part][G, U][rows][n]; 0: none do
     float *work;
 };
 
@@ -40,7 +40,7 @@ struct tile_out {
 template <bool GATED>
 __device__ __forceinline__ void store_tile(const tile_out &t, int64_t rows, int64_t n, uint8_t *lds, const f32x4 (&acc)[8][8], int64_t m0, int64_t n0, int part)
 {
-    const bool split = t.parts > 1;
+    const bool split = t.parts > 0;
     if constexpr (!GATED) store_sums(split ? part_of(t.work, part, rows, n) : t.y, rows, n, acc, m0, n0);
     else {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, chunk = lane % 16 * 2;
@@ -271,58 +271,100 @@ __global__ __launch_bounds__(256) void wide_tile_kernel(wide_args t, tile_out ou
         static_assert(sizeof(wide_args) % 8 == 0 && alignof(tile_out) <= 8, "where the second argument starts");
         const tile_out &out = argument<tile_out>(sizeof(wide_args));
         if constexpr (GATED) store_tile<GATED>(out, t.rows, t.cols, lds, acc, u.i0, u.j0, u.part);
-        else store_sums(out.parts > 1 ? part_of(out.work, u.part, t.rows, t.cols) : out.y, t.rows, t.cols, acc, u.i0, u.j0);
+        else store_sums(out.parts ? part_of(out.work, u.part, t.rows, t.cols) : out.y, t.rows, t.cols, acc, u.i0, u.j0);
     });
 }
 
-int64_t tiles_of(int64_t m, int64_t n, bool gated) { return ((m + 255) / 256) * ((n + (gated ? 127 : 255)) / (gated ? 128 : 256)); }
-
-int parts_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide)
-{
-    const int64_t values = m * n * (gated ? 2 : 1), tiles = tiles_of(m, n, gated);
-    if (!wide) return fp8_parts(tiles, (k + 4 * kFp8Block - 1) / (4 * kFp8Block), 4 * kByteStepUs, values);       // (parts of whole runs of four blocks, the words of their exponents)
-    return gated ? fp8_parts(tiles, (k + kWideStep - 1) / kWideStep, kWideStepUs, values) : wide_plan(m, n, k, 1, 1).parts;
-}
-
-size_t work_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide)
-{
-    const int parts = parts_of(m, n, k, gated, wide);
-    return parts > 1 ? (size_t)parts * (gated ? 2 : 1) * m * n * 4 : 0;
-}
-
+// in tiles of 64 x 64 (GATED: of 32 hidden units)
 template <bool GATED>
-hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_blocks &up, tile_out &out, bool wide, hipStream_t s)
+__global__ __launch_bounds__(256, 4) void small_kernel(wide_args t, tile_out out)
+{
+    __shared__ __align__(16) uint8_t lds[kSmallLds];
+    small_tile<WIDE_PRODUCT, GATED>(t, lds, [&](const wide_unit &u, int64_t row, int64_t col, f32x4 first, f32x4 second) {
+        if constexpr (!GATED) {
+            const fp8_matrix y = out.work ? part_of(out.work, u.part, t.rows, t.cols) : out.y;
+            store_four(y, row, col, t.cols, first);
+            store_four(y, row, col + 16, t.cols, second);
+        } else if (out.work) {
+            store_four(part_of(out.work, 2 * u.part, t.rows, t.cols), row, col, t.cols, first);
+            store_four(part_of(out.work, 2 * u.part + 1, t.rows, t.cols), row, col, t.cols, second);
+        } else {
+            f32x4 h;
+#pragma unroll
+            for (int e = 0; e < 4; e++) h[e] = (out.gated.act == PVQ_SILU ? act_value<PVQ_SILU>(first[e]) : act_value<PVQ_GELU>(first[e])) * second[e];
+            store_four(out.gated.h, row, col, t.cols, h);
+        }
+    });
+}
+
+// The tiles of a product, rows of 0 for those on the 8-bit instruction; join: whether the sums go to work, to be added there or taken to blocks.
+struct product_plan {
+    wide_tiles tiles;
+    bool join;
+};
+
+product_plan plan_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide, bool to_blocks)
+{
+    if (wide && !gated) {
+        const wide_tiles t = wide_plan(m, n, k, 1, 1);
+        return {t, t.parts > 1};
+    }
+    const int64_t values = m * n * (gated ? 2 : 1), tiles = (m + 255) / 256 * ((n + (gated ? 127 : 255)) / (gated ? 128 : 256)), steps = (k + kWideStep - 1) / kWideStep;
+    wide_tiles large{wide ? 256 : 0, 256, 1, 0.0}, small{64, gated ? 32 : 64, 1, 0.0};
+    // (8-bit: parts of whole runs of four blocks, the words of their exponents)
+    large.parts = wide ? fp8_parts(tiles, steps, kWideStepUs, values, &large.us) : fp8_parts(tiles, (k + 4 * kFp8Block - 1) / (4 * kFp8Block), 4 * kByteStepUs, values, &large.us);
+    small.parts = fp8_small_parts((m + 63) / 64 * ((n + small.cols - 1) / small.cols), steps, values, to_blocks, &small.us);
+    if (to_blocks) large.us += 15.0 * (double)((tiles * large.parts + 255) / 256);              // (the codes of its epilogue)
+    if (k && small.us < large.us) return {small, small.parts > 1 || to_blocks};
+    return {large, large.parts > 1};
+}
+
+size_t work_of(int64_t m, int64_t n, int64_t k, bool gated, bool wide, bool to_blocks)
+{
+    const product_plan plan = plan_of(m, n, k, gated, wide, to_blocks);
+    return plan.join ? (size_t)plan.tiles.parts * (gated ? 2 : 1) * m * n * 4 : 0;
+}
+
+// out.parts becomes 0 where there is nothing to join
+template <bool GATED>
+hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_blocks &up, tile_out &out, bool wide, bool to_blocks, hipStream_t s)
 {
     const int64_t m = a.rows, n = b.rows, k = a.cols;
-    out.parts = k ? parts_of(m, n, k, GATED, wide) : 1;
-    const dim3 grid((unsigned)tiles_of(m, n, GATED), (unsigned)out.parts);
+    const product_plan plan = plan_of(m, n, k, GATED, wide, to_blocks);
     constexpr int kLds = 2 * 2 * 256 * (kFp8Block + 4);
     auto allow = [](auto kernel, int bytes) { return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    if (!wide) {
-        const hipError_t e = allow(&tile_kernel<GATED>, kLds);
-        if (e != hipSuccess) return e;
-        tile_args t{a, b, up, n, (int)((m + 255) / 256), 0, 0};
-        t.tiles_n = (int)(grid.x / t.tiles_m);
-        t.blocks_a_part = (int)(((a.blocks() + 3) / 4 + out.parts - 1) / out.parts * 4);
-        hipLaunchKernelGGL(tile_kernel<GATED>, grid, dim3(256), kLds, s, t, out);
-        return hipGetLastError();
+    out.parts = plan.join ? plan.tiles.parts : 0;
+    if (!plan.join) out.work = nullptr;
+    if (plan.tiles.rows == 0 || (GATED && plan.tiles.rows == 256)) {
+        const int64_t across = (n + (GATED ? 127 : 255)) / (GATED ? 128 : 256), down = (m + 255) / 256;
+        const dim3 grid((unsigned)(down * across), (unsigned)plan.tiles.parts);
+        if (!wide) {
+            const hipError_t e = allow(&tile_kernel<GATED>, kLds);
+            if (e != hipSuccess) return e;
+            const tile_args t{a, b, up, n, (int)down, (int)across, (int)(((a.blocks() + 3) / 4 + plan.tiles.parts - 1) / plan.tiles.parts * 4)};
+            hipLaunchKernelGGL(tile_kernel<GATED>, grid, dim3(256), kLds, s, t, out);
+            return hipGetLastError();
+        }
     }
     wide_args t{};
     t.a = a; t.b[0] = b; t.b[1] = up;
     t.rows = m; t.cols = n; t.depth = k; t.terms = 1;
+    wide_tiles tiles = plan.tiles;
+    if (GATED && tiles.rows == 256) tiles.cols = 128;           // (hidden units)
+    t.use(tiles, 1);
+    if (tiles.rows == kSmallTile) {
+        hipLaunchKernelGGL(small_kernel<GATED>, dim3((unsigned)t.units), dim3(256), 0, s, t, out);
+        return hipGetLastError();
+    }
+    hipError_t e;
     if constexpr (GATED) {
-        const hipError_t e = allow(&wide_tile_kernel<true, 8>, kWideLds);
+        e = allow(&wide_tile_kernel<true, 8>, kWideLds);
         if (e != hipSuccess) return e;
-        t.parts = out.parts;
-        t.tiles_i = (int)((m + 255) / 256); t.tiles_j = (int)(grid.x / t.tiles_i);
-        t.steps_a_part = (int)(((k + kWideStep - 1) / kWideStep + t.parts - 1) / t.parts);
-        t.units = (int)(grid.x * grid.y);
         hipLaunchKernelGGL((wide_tile_kernel<true, 8>), dim3((unsigned)t.units), dim3(256), kWideLds, s, t, out);
     } else {
-        const auto kernel = t.use(1).low ? &wide_tile_kernel<false, 4> : &wide_tile_kernel<false, 8>;
-        const hipError_t e = allow(kernel, kWideLds);
+        const auto kernel = tiles.rows == 128 ? &wide_tile_kernel<false, 4> : &wide_tile_kernel<false, 8>;
+        e = allow(kernel, kWideLds);
         if (e != hipSuccess) return e;
-        out.parts = t.parts;
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(t.units, 256)), dim3(256), kWideLds, s, t, out);
     }
     return hipGetLastError();
@@ -330,15 +372,15 @@ hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_bloc
 
 }  // namespace
 
-size_t fp8_product_work(int64_t m, int64_t n, int64_t k, int out_dtype) { return fp8_rows_pay(m) ? 0 : work_of(m, n, k, false, out_dtype == PVQ_F32); }
-size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide) { return work_of(m, n, k, true, wide); }
+size_t fp8_product_work(int64_t m, int64_t n, int64_t k, int out_dtype) { return fp8_rows_pay(m) ? 0 : work_of(m, n, k, false, out_dtype == PVQ_F32, false); }
+size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide, bool to_blocks) { return work_of(m, n, k, true, wide, to_blocks); }
 
 hipError_t fp8_launch_product(const fp8_product_args &p, hipStream_t s)
 {
     tile_out out{};
     out.y = p.y; out.work = p.work;
-    hipError_t e = launch_tiles<false>(p.a, p.b, {}, out, p.y.dtype == PVQ_F32, s);
-    if (out.parts > 1 && e == hipSuccess) e = fp8_launch_join(p.work, out.parts, p.a.rows, p.b.rows, p.y, s);
+    hipError_t e = launch_tiles<false>(p.a, p.b, {}, out, p.y.dtype == PVQ_F32, false, s);
+    if (out.parts && e == hipSuccess) e = fp8_launch_join(p.work, out.parts, p.a.rows, p.b.rows, p.y, s);
     return e;
 }
 
@@ -350,7 +392,7 @@ hipError_t fp8_launch_gated(const fp8_gated_args &g, hipStream_t s)
     // Kept products are codes of sums of 32 bits: what the 8-bit instructions are off would change one code of 2000, which is as
     // much again as the roundings of the gradients to bfloat16 (dX 3.0e-3 off instead of 2.3e-3).
     const bool wide = g.gc || (g.h.data && g.h.dtype == PVQ_F32);
-    hipError_t e = launch_tiles<true>(g.x, g.gate, g.up, out, wide, s);
-    if (out.parts > 1 && e == hipSuccess) e = fp8_launch_gated_join(g.work, out.parts, g, s);
+    hipError_t e = launch_tiles<true>(g.x, g.gate, g.up, out, wide, g.gc || g.hc, s);
+    if (out.parts && e == hipSuccess) e = fp8_launch_gated_join(g.work, out.parts, g, s);
     return e;
 }

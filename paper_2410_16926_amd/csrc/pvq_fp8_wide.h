@@ -15,19 +15,22 @@ enum wide_kind {
     WIDE_WEIGHT_GRAD,    // A(i, r) = dy[r][i], B(r, j) = b[r][j]
 };
 
-// Tiles of 256 x 256, or low ones of 128 x 256 where these take less: a step of them is 64 matrix instructions less but the same codes to decode.
+// Tiles of 256 x 256, low ones of 128 x 256, or small ones of 64 x 64 (pvq_fp8_small.h), whichever take less: a step of a low tile is 64 matrix
+// instructions less but the same codes to decode.
 struct wide_tiles {
-    bool low;
-    int parts;
-    int rows() const { return low ? 128 : 256; }
+    int rows, cols, parts;
+    double us;
 };
 inline wide_tiles wide_plan(int64_t rows, int64_t cols, int64_t depth, int terms, int outputs)
 {
-    const int64_t across = (cols + kWideTile - 1) / kWideTile * outputs, steps = (depth + kWideStep - 1) / kWideStep * terms, values = rows * cols * outputs;
-    double us, low_us;
-    const int parts = fp8_parts((rows + 255) / 256 * across, steps, kWideStepUs, values, &us), low_parts = fp8_parts((rows + 127) / 128 * across, steps, kLowStepUs, values, &low_us);
-    const bool low = low_us < us;
-    return {low, low ? low_parts : parts};
+    const int64_t steps = (depth + kWideStep - 1) / kWideStep * terms, values = rows * cols * outputs;
+    auto tiles = [&](int r, int c) { return (rows + r - 1) / r * ((cols + c - 1) / c) * outputs; };
+    wide_tiles best{256, 256, 1, 0.0}, low{128, 256, 1, 0.0}, small{64, 64, 1, 0.0};
+    best.parts = fp8_parts(tiles(256, 256), steps, kWideStepUs, values, &best.us);
+    low.parts = fp8_parts(tiles(128, 256), steps, kLowStepUs, values, &low.us);
+    small.parts = fp8_small_parts(tiles(64, 64), steps, values, false, &small.us);
+    if (low.us < best.us) best = low;
+    return small.us < best.us ? small : best;
 }
 
 struct wide_args {
@@ -40,19 +43,40 @@ struct wide_args {
     int parts, steps_a_part;         // of a split sum, whose parts go to work
     int units;                       // tiles of all parts of all outputs
 
-    // the tiles that wide_plan takes
-    wide_tiles use(int outputs)
+    // these tiles of that many outputs
+    void use(const wide_tiles &plan, int outputs)
     {
-        const wide_tiles plan = wide_plan(rows, cols, depth, terms, outputs);
         parts = plan.parts;
-        tiles_i = (int)((rows + plan.rows() - 1) / plan.rows());
-        tiles_j = (int)((cols + kWideTile - 1) / kWideTile);
+        tiles_i = (int)((rows + plan.rows - 1) / plan.rows);
+        tiles_j = (int)((cols + plan.cols - 1) / plan.cols);
         steps_a_part = (int)(((depth + kWideStep - 1) / kWideStep * terms + parts - 1) / parts);
         units = tiles_i * tiles_j * outputs * parts;
-        return plan;
     }
     float *work;
 };
+
+// Where a step's part of an operand's tile starts, and how many bytes of the matrix are left there, the upper word below zero where none are: what
+// lies behind is zero.  (Of 64 bits compared whole the vector unit does it, between matrix instructions.)
+struct source {
+    const uint8_t *p;
+    uint32_t left;
+    int32_t left_up;
+};
+__device__ inline source source_of(const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at)
+{
+    const int64_t left = (rows - 1) * row + row_bytes - at;
+    return source{(const uint8_t *)base + at, (uint32_t)left, (int32_t)(left >> 32)};
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t take(source &s, uint32_t step)       // the buffer of a step, and on to the next, `step` bytes on
+{
+    asm("" : "+s"(s.left_up));
+    const uint32_t left = s.left_up > 0 ? ~0u : s.left_up < 0 ? 0u : s.left;
+    const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, left, 0x00020000);
+    s.p += step;
+    s.left_up -= s.left < step;
+    s.left -= step;
+    return r;
+}
 
 // A tile, or a part of its sum: steps first .. last of output out_of at i0, j0.
 struct wide_unit {
@@ -102,17 +126,6 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
     u32x2 rb[kPieces];
     uint32_t re[kPieces];
     bf16x8 decoded[kPieces];         // A's codes, or else B's, for the next half
-    // Where a step's part of an operand's tile starts, and how many bytes of the matrix are left there, the upper word below zero where none are: what
-    // lies behind is zero.  (Of 64 bits compared whole the vector unit does it, between matrix instructions.)
-    struct source {
-        const uint8_t *p;
-        uint32_t left;
-        int32_t left_up;
-    };
-    auto source_of = [](const void *base, int64_t row, int64_t rows, int64_t row_bytes, int64_t at) {
-        const int64_t left = (rows - 1) * row + row_bytes - at;
-        return source{(const uint8_t *)base + at, (uint32_t)left, (int32_t)(left >> 32)};
-    };
     source a_src, b_src, u_src, ae_src, be_src, ue_src;
     auto stop = [&] { a_src.left_up = b_src.left_up = u_src.left_up = ae_src.left_up = be_src.left_up = ue_src.left_up = -1; };
     // where the loads are
@@ -147,15 +160,6 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         ahead_left = max((KIND == WIDE_INPUT_GRAD && !term ? min(steps_a_term, ahead.last + 1) : ahead.last + 1) - step, 1);
     };
     __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
-    auto take = [](source &s, uint32_t step) {       // the buffer of a step, and on to the next, `step` bytes on
-        asm("" : "+s"(s.left_up));
-        const uint32_t left = s.left_up > 0 ? ~0u : s.left_up < 0 ? 0u : s.left;
-        const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, left, 0x00020000);
-        s.p += step;
-        s.left_up -= s.left < step;
-        s.left -= step;
-        return r;
-    };
     // (rows along the sum: an exponent is that of two steps)
     const uint32_t a_step = A_CODES ? kWideStep : A_ALONG ? kWideStep * 2 : kWideStep * a_row, b_step = B_ALONG ? kWideStep : kWideStep * b_row;
     auto aim_a = [&](int what) {

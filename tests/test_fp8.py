@@ -128,12 +128,14 @@ def test_the_gated_block_refuses():
         assert f(A16, 8, 2, 8, 5, None) == f(A16, 8, 2, -8, 5, C.byref(need)) == INVALID
         assert f(A16, 1 << 23, 1, (1 << 22) + 1, 5, C.byref(need)) == UNSUPPORTED
         assert f(A16, 64, 2, 64, 5, C.byref(need)) == 0 and need.value == 0
-        assert f(A16 + 2, 8, 2, 8, 5, C.byref(need)) == 0 and need.value >= 2 * 8 * 2        # rows that do not start at 16 bytes
-        assert f(A16, 9, 2, 8, 5, C.byref(need)) == 0 and need.value >= 2 * 8 * 2
+        # rows that do not start at 16 bytes: small ones are taken as they are
+        assert f(A16 + 2, 8, 2, 8, 5, C.byref(need)) == f(A16, 9, 2, 8, 5, C.byref(need)) == 0 and need.value == 0
+        assert f(A16 + 2, 4096, 4096, 4096, 4096, C.byref(need)) == 0 and need.value >= 4096 * 4096 * 2
+        assert f(A16, 4097, 4096, 4096, 4096, C.byref(need)) == 0 and need.value >= 4096 * 4096 * 2
     size = need.value
     for work, n, want in ((None, 1 << 40, INVALID), (A16, size - 1, INVALID), (A16 + 8, 1 << 40, ALIGNMENT)):
-        assert L.pvq_fp8_input_grad(A16, 9, 2, A16, A16, 8, 5, A16, F32, 5, work, n, None) == want
-        assert L.pvq_fp8_weight_grad(A16, 9, 2, 8, A16, A16, 5, A16, F32, 5, work, n, None) == want
+        assert L.pvq_fp8_input_grad(A16, 4097, 4096, A16, A16, 4096, 4096, A16, F32, 4096, work, n, None) == want
+        assert L.pvq_fp8_weight_grad(A16, 4097, 4096, 4096, A16, A16, 4096, A16, F32, 4096, work, n, None) == want
     assert L.pvq_fp8_product_work_bytes(100, 100, 100000, BF16, C.byref(need)) == 0 and need.value > 0     # few tiles, a long sum: split
     assert L.pvq_fp8_product(A16, A16, 100, A16, A16, 100, 100000, A16, BF16, 100, None, 0, None) == INVALID
     assert L.pvq_fp8_product(A16, A16, 100, A16, A16, 100, 100000, A16, BF16, 100, A16, need.value - 1, None) == INVALID

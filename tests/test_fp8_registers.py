@@ -9,7 +9,7 @@ import pytest
 from paper_2410_16926_amd import build
 
 CSRC = os.path.join(os.path.dirname(os.path.abspath(build.__file__)), "csrc")
-KERNEL = re.compile(r"^(_ZN\S*?(?:wide_tile_kernel|tile_kernel|grad_kernel)\S*):", re.M)
+KERNEL = re.compile(r"^(_ZN\S*?\d(?:wide_tile_kernel|tile_kernel|grad_kernel)\S*):", re.M)
 
 
 @pytest.mark.parametrize("name,kernels", [("pvq_fp8_grad.hip", 4), ("pvq_fp8_product.hip", 5)])

@@ -510,14 +510,19 @@ def test_offsets_beyond_32_bits():
     """Planes and results of more than 4 GiB: the last rows are those of a small call."""
     m, n, k = 40, 70, 384
     rng = np.random.default_rng(8)
-    X, W = blocks(*ref.random_blocks(rng, m, k)[:2], k), blocks(*ref.random_blocks(rng, n, k)[:2], k)
+    (xc, xe, x), (wc, we, w) = ref.random_blocks(rng, m, k), ref.random_blocks(rng, n, k)
+    X, W = blocks(xc, xe, k), blocks(wc, we, k)
     rows = (1 << 32) // k + 1000
     codes, exps = torch.zeros(rows, k, dtype=torch.uint8, device="cuda"), torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda")
     codes[-n:], exps[-n:] = W.codes, W.exponents
     LONG = pvq.Fp8Blocks(rows, k, codes, exps)
-    want = pvq.pvq_fp8_product(X, W, torch.bfloat16)
-    got = pvq.pvq_fp8_product(X, LONG, torch.bfloat16)                  # few rows
-    assert torch.equal(got[:, -n:], want) and not got[:, :1000].any()
+    # (which instruction forms the sums depends on the shape: both are as far from the 64-bit ones as the 8-bit one may be)
+    got, want = pvq.pvq_fp8_product(X, LONG, torch.bfloat16), pvq.pvq_fp8_product(X, W, torch.bfloat16)
+    for v in (got[:, -n:], want):
+        check_sum(v, x @ w.T, np.abs(x) @ np.abs(w).T, k, "bf16", True, np.sqrt((x * x) @ (w * w).T))
+    assert not got[:, :1000].any()
+    X = pvq.Fp8Blocks(7, k, X.codes[:7], X.exponents[:7])
+    assert torch.equal(pvq.pvq_fp8_product(X, LONG, torch.bfloat16)[:, -n:], pvq.pvq_fp8_product(X, W, torch.bfloat16))      # few rows
     del got
     got = pvq.pvq_fp8_product(LONG, W, torch.bfloat16)                  # tiles, and a result of 1.5 GiB
     want = pvq.pvq_fp8_product(pvq.Fp8Blocks(n, k, W.codes, W.exponents), W, torch.float32)

@@ -11,9 +11,10 @@ from tests import test_gpu_fp8 as base
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
+# (also small tiles against large ones: up to some 10^10 operations, or where large ones would be few)
 # few tiles of a long sum; either side of 8, 16 and 32 rows; a tile and one row more; 274 tiles of few rows and 289 of many
 PRODUCTS = [(33, 100, 20011), (70, 300, 20011), (300, 260, 6000), (8, 40, 1300), (9, 40, 1300), (16, 33, 20011), (32, 513, 1025), (33, 513, 1025),
-            (128, 256, 513), (129, 257, 512), (256, 256, 640), (257, 255, 641), (100, 70001, 130), (4352, 4100, 130)]
+            (128, 256, 513), (129, 257, 512), (256, 256, 640), (257, 255, 641), (100, 70001, 130), (4352, 4100, 130), (333, 3001, 11008), (1024, 3000, 2048), (700, 2050, 3001)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
@@ -22,7 +23,8 @@ def test_products(m, n, k, dtype):
     base.test_product(m, n, k, dtype)
 
 
-@pytest.mark.parametrize("m,n,k,act", [(70, 200, 9000, "silu"), (40, 129, 5000, "gelu"), (32, 260, 4100, "silu"), (300, 17000, 129, "gelu")])
+@pytest.mark.parametrize("m,n,k,act", [(70, 200, 9000, "silu"), (40, 129, 5000, "gelu"), (32, 260, 4100, "silu"), (300, 17000, 129, "gelu"), (300, 3000, 4000, "silu"),
+                                         (1100, 2100, 640, "gelu"), (20, 4000, 300, "gelu")])
 def test_gated(m, n, k, act):
     base.test_gated(m, n, k, act)
 
@@ -30,13 +32,15 @@ def test_gated(m, n, k, act):
 # dX and dW of each: either's sum long and its tiles few; many tiles of few rows, and of many
 @pytest.mark.parametrize("m,n,k,dtype,gap,shift", [(70, 20011, 300, "f32", 0, 0), (70, 20011, 300, "bf16", 5, 1), (20011, 70, 300, "f16", 0, 0),
                                                    (20011, 72, 300, "f32", 8, 0), (100, 130, 70001, "bf16", 0, 0), (4352, 64, 4100, "f32", 0, 0),
-                                                   (65, 4352, 4100, "bf16", 3, 1), (128, 128, 256, "f16", 0, 0), (129, 192, 257, "f32", 0, 0)])
+                                                   (65, 4352, 4100, "bf16", 3, 1), (128, 128, 256, "f16", 0, 0), (129, 192, 257, "f32", 0, 0),
+                                                   (333, 3001, 2100, "bf16", 0, 0), (700, 1100, 3000, "f32", 5, 1), (517, 2000, 2048, "bf16", 8, 0), (64, 63, 65, "f32", 1, 0),
+                                                   (63, 65, 64, "bf16", 0, 1), (1500, 1500, 1500, "f16", 4, 0)])
 def test_gradients_of_a_product(m, n, k, dtype, gap, shift):
     base.test_gradients_of_a_product(m, n, k, dtype, gap, shift)
 
 
 @pytest.mark.parametrize("m,n,k,act,dtype", [(70, 9000, 129, "silu", "f32"), (9000, 70, 129, "gelu", "bf16"), (100, 130, 35001, "silu", "bf16"),
-                                             (4352, 64, 4100, "gelu", "f32"), (65, 2304, 4100, "silu", "f16")])
+                                             (4352, 64, 4100, "gelu", "f32"), (65, 2304, 4100, "silu", "f16"), (500, 700, 3000, "gelu", "f32"), (1000, 2100, 1200, "silu", "bf16"), (64, 65, 4000, "silu", "f32")])
 def test_gated_backward(m, n, k, act, dtype):
     base.test_gated_backward(m, n, k, act, dtype)
 
