@@ -17,6 +17,10 @@ PRODUCTS = [(33, 100, 20011), (70, 300, 20011), (300, 260, 6000), (8, 40, 1300),
             (128, 256, 513), (129, 257, 512), (256, 256, 640), (257, 255, 641), (100, 70001, 130), (4352, 4100, 130), (333, 3001, 11008), (1024, 3000, 2048), (700, 2050, 3001)]
 
 
+# every kind of large tile: in one round or several, its sums whole or split
+PRODUCTS += [(1316, 4457, 66), (4892, 3288, 64), (72, 4359, 4739), (3550, 842, 65), (66, 4305, 4576), (3667, 2164, 64), (5063, 3203, 66), (4273, 265, 4714)]
+
+
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_products(m, n, k, dtype):
@@ -24,7 +28,9 @@ def test_products(m, n, k, dtype):
 
 
 @pytest.mark.parametrize("m,n,k,act", [(70, 200, 9000, "silu"), (40, 129, 5000, "gelu"), (32, 260, 4100, "silu"), (300, 17000, 129, "gelu"), (300, 3000, 4000, "silu"),
-                                         (1100, 2100, 640, "gelu"), (20, 4000, 300, "gelu")])
+                                         (1100, 2100, 640, "gelu"), (20, 4000, 300, "gelu"),
+                                         (82, 2052, 4799, "silu"), (68, 4737, 4996, "gelu"), (72, 4156, 2998, "gelu"), (132, 5637, 4311, "silu"),
+                                         (1364, 5712, 64, "silu"), (2306, 1250, 65, "gelu"), (2578, 937, 64, "silu")])
 def test_gated(m, n, k, act):
     base.test_gated(m, n, k, act)
 
@@ -34,13 +40,19 @@ def test_gated(m, n, k, act):
                                                    (20011, 72, 300, "f32", 8, 0), (100, 130, 70001, "bf16", 0, 0), (4352, 64, 4100, "f32", 0, 0),
                                                    (65, 4352, 4100, "bf16", 3, 1), (128, 128, 256, "f16", 0, 0), (129, 192, 257, "f32", 0, 0),
                                                    (333, 3001, 2100, "bf16", 0, 0), (700, 1100, 3000, "f32", 5, 1), (517, 2000, 2048, "bf16", 8, 0), (64, 63, 65, "f32", 1, 0),
-                                                   (63, 65, 64, "bf16", 0, 1), (1500, 1500, 1500, "f16", 4, 0)])
+                                                   (63, 65, 64, "bf16", 0, 1), (1500, 1500, 1500, "f16", 4, 0),
+                                                   (65, 661, 4588, "f32", 0, 0), (65, 2834, 5480, "bf16", 3, 1), (4658, 72, 4110, "f16", 0, 0), (5626, 66, 522, "f32", 0, 0),
+                                                   (2898, 74, 5597, "bf16", 0, 0), (69, 4967, 4331, "f32", 1, 0), (5513, 72, 1291, "f16", 8, 0), (3132, 65, 5179, "f32", 0, 0),
+                                                   (4208, 5227, 260, "bf16", 0, 0), (69, 4697, 3398, "f32", 8, 0), (5502, 4242, 258, "f32", 0, 1)])
 def test_gradients_of_a_product(m, n, k, dtype, gap, shift):
     base.test_gradients_of_a_product(m, n, k, dtype, gap, shift)
 
 
 @pytest.mark.parametrize("m,n,k,act,dtype", [(70, 9000, 129, "silu", "f32"), (9000, 70, 129, "gelu", "bf16"), (100, 130, 35001, "silu", "bf16"),
-                                             (4352, 64, 4100, "gelu", "f32"), (65, 2304, 4100, "silu", "f16"), (500, 700, 3000, "gelu", "f32"), (1000, 2100, 1200, "silu", "bf16"), (64, 65, 4000, "silu", "f32")])
+                                             (4352, 64, 4100, "gelu", "f32"), (65, 2304, 4100, "silu", "f16"), (500, 700, 3000, "gelu", "f32"), (1000, 2100, 1200, "silu", "bf16"), (64, 65, 4000, "silu", "f32"),
+                                             (64, 5138, 270, "gelu", "bf16"), (75, 2309, 3120, "silu", "f32"), (4774, 65, 2185, "gelu", "f16"), (66, 4279, 801, "silu", "f32"),
+                                             (65, 4609, 1625, "gelu", "bf16"), (2857, 4108, 67, "silu", "bf16"), (5626, 66, 522, "gelu", "f32"), (2898, 74, 5597, "silu", "bf16"),
+                                             (74, 2414, 4227, "gelu", "f32"), (5513, 72, 1291, "silu", "f16"), (3132, 65, 5179, "silu", "f32"), (5471, 3078, 65, "gelu", "f32")])
 def test_gated_backward(m, n, k, act, dtype):
     base.test_gated_backward(m, n, k, act, dtype)
 
