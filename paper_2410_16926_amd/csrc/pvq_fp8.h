@@ -70,7 +70,7 @@ inline int fp8_small_parts(int64_t tiles, int64_t steps, int64_t values, bool jo
         if (parts > 1 || join) us += 4.0 + 8.0 * parts * (double)values / 4e6;
         if (parts == 1 || us < least) { best = parts; least = us; }
     }
-    *takes = least;
+    *takes = tiles > (1 << 20) ? 1e30 : least;                      // (a launch has less than 2^32 threads)
     return best;
 }
 

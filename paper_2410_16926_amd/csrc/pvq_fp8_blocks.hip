@@ -117,17 +117,17 @@ __global__ __launch_bounds__(kThreads) void slopes_kernel(fp8_bf16 dh, fp8_block
 __global__ __launch_bounds__(kThreads) void join_kernel(const float *work, int parts, int64_t rows, int64_t cols, fp8_matrix out)
 {
     const int64_t runs = (cols + 3) / 4, total = rows * runs, part = rows * cols;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= total) return;
-    const int64_t row = i / runs, c = (i - row * runs) * 4, count = cols - c;
-    const float *p = work + row * cols + c;
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < parts; k++, p += part)
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / runs, c = (i - row * runs) * 4, count = cols - c;
+        const float *p = work + row * cols + c;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < parts; k++, p += part)
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-            if (j < count) sum[j] += p[j];
-    const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    store_values(out, row, c, count, v);
+            for (int j = 0; j < 4; j++)
+                if (j < count) sum[j] += p[j];
+        const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+        store_values(out, row, c, count, v);
+    }
 }
 
 // The parts' sums of G and U, [part][G, U][rows][cols], added, and what the gated block makes of them: sixteen lanes a block.
@@ -205,7 +205,7 @@ hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, cons
 
 hipError_t fp8_launch_join(const float *work, int parts, int64_t rows, int64_t cols, const fp8_matrix &out, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((rows * ((cols + 3) / 4) + kThreads - 1) / kThreads);
+    const unsigned grid = grid_for((rows * ((cols + 3) / 4) + kThreads - 1) / kThreads, 256 * 8 * 4);
     hipLaunchKernelGGL(join_kernel, dim3(grid), dim3(kThreads), 0, s, work, parts, rows, cols, out);
     return hipGetLastError();
 }

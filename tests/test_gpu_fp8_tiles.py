@@ -57,6 +57,15 @@ def test_gated_backward(m, n, k, act, dtype):
     base.test_gated_backward(m, n, k, act, dtype)
 
 
+@pytest.mark.parametrize("m,n", [(3, 5), (3001, 4001)])
+def test_empty_sums_fill_the_result(m, n):
+    none = [pvq.pvq_fp8_encode(torch.zeros(r, 0, device="cuda")) for r in (m, n)]
+    for t in ("f32", "bf16"):
+        out = base.matrix(np.ones((m, n)), t, 3, 1)
+        assert not pvq.pvq_fp8_product(*none, out=out).any()
+        assert torch.isnan(torch.as_strided(out, (m - 1, 3), (n + 3, 1), 1 + n)).all()
+
+
 @pytest.mark.parametrize("m", [5, 70])
 def test_nothing_is_taken_from_behind_the_last_exponent(m):
     """Three blocks of a row have four bytes of exponents: the fourth counts for nothing."""
