@@ -393,10 +393,12 @@ int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m,
 
 /*
  * Its backward pass, from dH (device, bfloat16 [m][lddh]), the block's inputs and the kept G and U:
- *   dU = dH * act(G),  dG = dH * U * act'(G)   (float32, rounded once to bfloat16 for the matrix instructions)
+ *   dU = dH * act(G),  dG = dH * U * act'(G)   (float32)
  *   dX = dG Wg + dU Wu  [m][lddx],   dWg = dG^T X  [n][lddw],   dWu = dU^T X  [n][lddw]   of out_dtype
- * dX may be NULL, or dWg and dWu both (what is not wanted is not computed).
- *   work   device, 16-byte aligned scratch of pvq_fp8_gated_backward_work_bytes bytes
+ * The matrix instructions take dG and dU in bfloat16: rounded once where out_dtype is PVQ_BF16 (off by half a step, as the results are), otherwise as
+ * a sum of two, the rounding and what it left (2^-16 of a value at most), which takes twice the operations.  A dG or dU that rounds out of
+ * bfloat16's range is infinite.  dX may be NULL, or dWg and dWu both (what is not wanted is not computed).
+ *   work   device, 16-byte aligned scratch of pvq_fp8_gated_backward_work_bytes bytes (enough for every out_dtype)
  */
 int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes);
 int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_t *x_codes, const uint8_t *x_exponents, int64_t m,

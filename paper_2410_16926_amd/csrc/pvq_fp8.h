@@ -108,11 +108,11 @@ struct fp8_bf16 {
     int64_t rows = 0, cols = 0, ld = 0;
 };
 
-// out[p] = sum over the terms t of term(t): dX = sum_t dY_t W_t (transposed == false; one output, one or two terms) or
-// dW_p = dY_p^T X_p (transposed == true; one or two outputs of one term each)
+// dX = sum over p of dY_p W_p (one output) or dW_p = dY_p^T X_p (an output each), of one or two pairs.  A dY may be given in pieces whose sum it is:
+// its rounding to bfloat16 and that of what was left.
 struct fp8_grad_args {
-    int pairs;
-    fp8_bf16 dy[2];
+    int pairs, pieces;
+    fp8_bf16 dy[4];              // pair p's piece i: dy[p * pieces + i], all of one shape and stride
     fp8_blocks b[2];
     fp8_matrix out[2];
     float *work;
@@ -120,15 +120,15 @@ struct fp8_grad_args {
 // whether a single gradient's dY is taken with rows that start and end anywhere
 bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k);
 bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k);
-size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
-size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs);
+size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
+size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
 hipError_t fp8_launch_input_grad(const fp8_grad_args &a, hipStream_t s);
 hipError_t fp8_launch_weight_grad(const fp8_grad_args &a, hipStream_t s);
 
 hipError_t fp8_launch_encode(const void *X, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes, uint8_t *exps, hipStream_t s);
 hipError_t fp8_launch_decode(const fp8_blocks &b, const fp8_matrix &y, hipStream_t s);
-// dG = dH U act'(G), dU = dH act(G) in bf16 with row strides of ld values, the columns from n to ld set to zero
-hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du,
+// dG = dH U act'(G), dU = dH act(G), each in one or two pieces of bf16, [piece][rows][ld], the columns from n to ld set to zero
+hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du, int pieces,
                                    int64_t ld, hipStream_t s);
 // a bf16 matrix to rows of `ld` values that start at 16 bytes, the columns behind the last zero
 hipError_t fp8_launch_align(const fp8_bf16 &from, uint16_t *to, int64_t ld, hipStream_t s);

@@ -77,15 +77,18 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(fp8_blocks b, fp8_matr
     }
 }
 
-// One lane a run of eight: dG = dH U act'(G) and dU = dH act(G).
-template <int ACT>
+// What the rounding of a value to bfloat16 left of it, exactly (nothing of an infinity or a NaN, or of what becomes one).
+__device__ inline float left_of(float v, uint32_t rounded) { return (rounded & 0x7F80u) == 0x7F80u ? 0.0f : v - __uint_as_float(rounded << 16); }
+
+// One lane a run of eight: dG = dH U act'(G) and dU = dH act(G), and with two pieces what their roundings left.
+template <int ACT, int PIECES>
 __global__ __launch_bounds__(kThreads) void slopes_kernel(fp8_bf16 dh, fp8_blocks g, fp8_blocks u, uint16_t *dg, uint16_t *du,
                                                           int64_t ld)
 {
-    const int64_t runs = ld / 8, total = dh.rows * runs, n = dh.cols, code_row = g.code_row(), exp_row = g.exp_row();
+    const int64_t runs = ld / 8, total = dh.rows * runs, n = dh.cols, code_row = g.code_row(), exp_row = g.exp_row(), piece = dh.rows * ld;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t row = i / runs, c = (i - row * runs) * 8;
-        u32x4 wg = {0, 0, 0, 0}, wu = {0, 0, 0, 0};
+        u32x4 wg[PIECES] = {}, wu[PIECES] = {};
         if (c < n) {
             float d[8];
             load8<PVQ_BF16>(dh.data + row * dh.ld, c, n, d);
@@ -104,12 +107,19 @@ __global__ __launch_bounds__(kThreads) void slopes_kernel(fp8_bf16 dh, fp8_block
                     og[j] = in ? d[2 * p + j] * (b[j] * su) * slope : 0.0f;
                     ou[j] = in ? d[2 * p + j] * value : 0.0f;
                 }
-                wg[p] = bf16_pair(og[0], og[1]);
-                wu[p] = bf16_pair(ou[0], ou[1]);
+                wg[0][p] = bf16_pair(og[0], og[1]);
+                wu[0][p] = bf16_pair(ou[0], ou[1]);
+                if constexpr (PIECES == 2) {
+                    wg[1][p] = bf16_pair(left_of(og[0], wg[0][p] & 0xFFFFu), left_of(og[1], wg[0][p] >> 16));
+                    wu[1][p] = bf16_pair(left_of(ou[0], wu[0][p] & 0xFFFFu), left_of(ou[1], wu[0][p] >> 16));
+                }
             }
         }
-        *reinterpret_cast<u32x4 *>(dg + row * ld + c) = wg;
-        *reinterpret_cast<u32x4 *>(du + row * ld + c) = wu;
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) {
+            *reinterpret_cast<u32x4 *>(dg + i * piece + row * ld + c) = wg[i];
+            *reinterpret_cast<u32x4 *>(du + i * piece + row * ld + c) = wu[i];
+        }
     }
 }
 
@@ -197,12 +207,13 @@ hipError_t fp8_launch_decode(const fp8_blocks &b, const fp8_matrix &y, hipStream
     return hipGetLastError();
 }
 
-hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du,
+hipError_t fp8_launch_gated_slopes(const fp8_bf16 &dh, const fp8_blocks &g, const fp8_blocks &u, int act, uint16_t *dg, uint16_t *du, int pieces,
                                    int64_t ld, hipStream_t s)
 {
     const unsigned grid = grid_for((dh.rows * (ld / 8) + kThreads - 1) / kThreads, 256 * 8 * 4);
-    if (act == PVQ_SILU) hipLaunchKernelGGL(slopes_kernel<PVQ_SILU>, dim3(grid), dim3(kThreads), 0, s, dh, g, u, dg, du, ld);
-    else hipLaunchKernelGGL(slopes_kernel<PVQ_GELU>, dim3(grid), dim3(kThreads), 0, s, dh, g, u, dg, du, ld);
+    const auto kernel = act == PVQ_SILU ? pieces == 1 ? &slopes_kernel<PVQ_SILU, 1> : &slopes_kernel<PVQ_SILU, 2>
+                                        : pieces == 1 ? &slopes_kernel<PVQ_GELU, 1> : &slopes_kernel<PVQ_GELU, 2>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, s, dh, g, u, dg, du, ld);
     return hipGetLastError();
 }
 

@@ -36,7 +36,9 @@ size_t work_of(int64_t rows, int64_t cols, int64_t depth, int terms, int outputs
 template <int KIND>
 hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t s)
 {
-    for (int i = 0; i < g.pairs; i++) { t.dy[i] = g.dy[i]; t.b[i] = g.b[i]; }
+    for (int i = 0; i < g.pairs * g.pieces; i++) t.dy[i] = g.dy[i];
+    for (int i = 0; i < g.pairs; i++) t.b[i] = g.b[i];
+    t.pieces = g.pieces;
     for (int i = 0; i < outputs; i++) t.out[i] = g.out[i];
     t.work = g.work;
     const wide_tiles plan = wide_plan(t.rows, t.cols, t.depth, t.terms, outputs);
@@ -61,19 +63,19 @@ hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t
 static bool as_it_is(const wide_tiles &plan) { return plan.rows == kSmallTile && plan.us < 14.0; }
 bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k) { return as_it_is(wide_plan(m, k, n, 1, 1)); }
 bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k) { return as_it_is(wide_plan(n, k, m, 1, 1)); }
-size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs) { return work_of(m, k, n, pairs, 1); }
-size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs) { return work_of(n, k, m, 1, pairs); }
+size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return work_of(m, k, n, pairs * pieces, 1); }
+size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return work_of(n, k, m, pieces, pairs); }
 
 hipError_t fp8_launch_input_grad(const fp8_grad_args &g, hipStream_t s)
 {
     wide_args t{};
-    t.rows = g.dy[0].rows; t.cols = g.b[0].cols; t.depth = g.dy[0].cols; t.terms = g.pairs;
+    t.rows = g.dy[0].rows; t.cols = g.b[0].cols; t.depth = g.dy[0].cols; t.terms = g.pairs * g.pieces;
     return launch<WIDE_INPUT_GRAD>(t, g, 1, s);
 }
 
 hipError_t fp8_launch_weight_grad(const fp8_grad_args &g, hipStream_t s)
 {
     wide_args t{};
-    t.rows = g.dy[0].cols; t.cols = g.b[0].cols; t.depth = g.dy[0].rows; t.terms = 1;
+    t.rows = g.dy[0].cols; t.cols = g.b[0].cols; t.depth = g.dy[0].rows; t.terms = g.pieces;
     return launch<WIDE_WEIGHT_GRAD>(t, g, g.pairs, s);
 }

@@ -51,6 +51,13 @@ int first_of(std::initializer_list<int> codes)
 // the row stride of a workspace's bfloat16 matrices, in values
 int64_t slope_row(int64_t n) { return (n + 63) / 64 * 64; }
 
+// Of how many pieces of bfloat16 the gated block's dG and dU are.  Rounded once they are off by half a step, 2^-8, which is what a result in
+// bfloat16 is off by anyway (2.3e-3 in all instead of 1.7e-3, in half the time).  A result of more bits takes a second piece, what the first left,
+// and is off by 2^-16 of a slope at most: float32 gradients of 517 x 2816 x 1024 by 2.5e-6 (one piece: 1.7e-3; float32 slopes: 4e-7 to 1e-6), float16
+// ones by no more than their own rounding, 2.1e-4 (1.7e-3).  2048 x 14336 x 4096 takes 1.6 ms with two pieces, 0.84 with one.
+int slope_pieces(int out_dtype) { return out_dtype == PVQ_BF16 ? 1 : 2; }
+constexpr int kMostPieces = 2;
+
 // Whether the gradient kernels of large tiles can take dY as it is: rows aligned to 16 bytes, a tile's within 32-bit offsets, and where they run along
 // the sum (dX) in whole steps of it.  Otherwise it is copied first, with zeros behind the rows.
 bool whole_rows(const void *dY, int64_t ld, int64_t n, bool along) { return aligned(dY, 16) && ld % 8 == 0 && ld <= kMostCols && (!along || n % 64 == 0); }
@@ -134,7 +141,7 @@ extern "C" int pvq_fp8_input_grad_work_bytes(const void *dY, int64_t lddy, int64
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, true) + fp8_input_grad_work(m, n, k, 1) : 0;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, true) + fp8_input_grad_work(m, n, k, 1, 1) : 0;
     return PVQ_OK;
 }
 
@@ -146,7 +153,7 @@ extern "C" int pvq_fp8_input_grad(const void *dY, int64_t lddy, int64_t m, const
     if (!known(out_dtype)) return PVQ_E_INVALID_ARG;
     if (m == 0 || k == 0) return PVQ_OK;
     fp8_grad_args a{};
-    a.pairs = 1;
+    a.pairs = a.pieces = 1;
     a.dy[0] = {(const uint16_t *)dY, m, n, lddy};
     a.b[0] = {w_codes, w_exponents, n, k};
     a.out[0] = {dX, out_dtype, lddx};
@@ -163,7 +170,7 @@ extern "C" int pvq_fp8_weight_grad_work_bytes(const void *dY, int64_t lddy, int6
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!bytes) return PVQ_E_INVALID_ARG;
-    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, false) + fp8_weight_grad_work(m, n, k, 1) : 0;
+    *bytes = m && n && k ? copy_bytes(dY, lddy, m, n, k, false) + fp8_weight_grad_work(m, n, k, 1, 1) : 0;
     return PVQ_OK;
 }
 
@@ -175,7 +182,7 @@ extern "C" int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int6
     if (!known(out_dtype)) return PVQ_E_INVALID_ARG;
     if (n == 0 || k == 0) return PVQ_OK;
     fp8_grad_args a{};
-    a.pairs = 1;
+    a.pairs = a.pieces = 1;
     a.dy[0] = {(const uint16_t *)dY, m, n, lddy};
     a.b[0] = {x_codes, x_exponents, m, k};
     a.out[0] = {dW, out_dtype, lddw};
@@ -226,9 +233,12 @@ extern "C" int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k
 {
     if (const int rc = first_of({check_shape(m, k), check_shape(n, k), check_shape(m, n)})) return rc;
     if (!bytes) return PVQ_E_INVALID_ARG;
-    const size_t slopes = up16((size_t)m * slope_row(n) * 2);
-    const size_t sums = m && n && k ? std::max(fp8_input_grad_work(m, n, k, 2), fp8_weight_grad_work(m, n, k, 2)) : 0;
-    *bytes = 2 * slopes + sums;
+    // (enough for every type of the results)
+    const size_t slopes = (size_t)m * slope_row(n) * 2;
+    size_t sums = 0;
+    for (int pieces = 1; m && n && k && pieces <= kMostPieces; pieces++)
+        sums = std::max({sums, fp8_input_grad_work(m, n, k, 2, pieces), fp8_weight_grad_work(m, n, k, 2, pieces)});
+    *bytes = 2 * kMostPieces * slopes + sums;
     return PVQ_OK;
 }
 
@@ -260,15 +270,14 @@ extern "C" int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_
         if (dWu && n && e == hipSuccess) e = fp8_launch_join(nullptr, 0, n, k, {dWu, out_dtype, lddw}, s);
         return status_of(e);
     }
-    const int64_t ld = slope_row(n);
-    const size_t slopes = up16((size_t)m * ld * 2);
-    uint16_t *dg = (uint16_t *)work, *du = (uint16_t *)((char *)work + slopes);
+    const int64_t ld = slope_row(n), slopes = m * ld;
     fp8_grad_args a{};
     a.pairs = 2;
-    a.dy[0] = {dg, m, n, ld};
-    a.dy[1] = {du, m, n, ld};
-    a.work = (float *)((char *)work + 2 * slopes);
-    e = fp8_launch_gated_slopes({(const uint16_t *)dH, m, n, lddh}, g, u, activation, dg, du, ld, s);
+    a.pieces = slope_pieces(out_dtype);
+    uint16_t *dg = (uint16_t *)work, *du = dg + a.pieces * slopes;
+    for (int i = 0; i < a.pairs * a.pieces; i++) a.dy[i] = {dg + i * slopes, m, n, ld};
+    a.work = (float *)(dg + 2 * kMostPieces * slopes);
+    e = fp8_launch_gated_slopes({(const uint16_t *)dH, m, n, lddh}, g, u, activation, dg, du, a.pieces, ld, s);
     if (dX && e == hipSuccess) {
         a.b[0] = gate; a.b[1] = up;
         a.out[0] = {dX, out_dtype, lddx};

@@ -33,17 +33,18 @@ __device__ __forceinline__ void small_sums(const wide_args &t, uint8_t *lds, con
     const uint16_t *y = nullptr;
     int64_t y_left = 0;                                         // of dY's row (along) or rows (across) from a thread's own on
     const int64_t y_cols = u.i0 + from < t.rows ? t.rows - u.i0 - from : 0;
-    int step = u.first;
+    int step = u.first, term_end = 0;
     auto start = [&] {
-        const int term = KIND == WIDE_INPUT_GRAD && step >= steps_a_term ? 1 : 0;
-        const bool second = (term | u.out_of) != 0;
+        const int term = term_of<KIND>(step, steps_a_term);
+        const bool second = second_pair<KIND>(t, term, u.out_of);
+        term_end = (term + 1) * steps_a_term;
         const int64_t r0 = (int64_t)(step - term * steps_a_term) * kWideStep;
         const fp8_blocks b = second || (GATED && wave >= 2) ? t.b[1] : t.b[0];
         if constexpr (A_CODES) {
             a_src = source_of(t.a.codes, a_row, t.rows, a_row, u.i0 * a_row + r0);
             ae_src = source_of(t.a.exps, ae_row, t.rows, ae_row, u.i0 * ae_row + r0 / kFp8Block);
         } else {
-            y = (second ? t.dy[1].data : t.dy[0].data) + ((A_ALONG ? u.i0 : r0) + row) * t.dy[0].ld + (A_ALONG ? r0 : u.i0) + from;
+            y = dy_of<KIND>(t, term, u.out_of).data + ((A_ALONG ? u.i0 : r0) + row) * t.dy[0].ld + (A_ALONG ? r0 : u.i0) + from;
             y_left = A_ALONG ? (u.i0 + row < t.rows ? t.depth - r0 - from : 0) : t.depth - r0 - row;
         }
         b_src = B_ALONG ? source_of(b.codes, b_row, b.rows, b_row, u.j0 * b_row + r0) : source_of(b.codes, b_row, t.depth, b_row, r0 * b_row + u.j0);
@@ -52,7 +53,7 @@ __device__ __forceinline__ void small_sums(const wide_args &t, uint8_t *lds, con
     start();
     // the next step, zeros behind the unit's last
     auto fetch = [&](piece &p) {
-        if (KIND == WIDE_INPUT_GRAD && step == steps_a_term) start();
+        if (KIND != WIDE_PRODUCT && step == term_end) start();
         if (step > u.last) { a_src.left_up = ae_src.left_up = b_src.left_up = be_src.left_up = -1; y_left = 0; }
         auto codes = [&](source &c, source &e, uint32_t c_step, uint32_t e_step, uint32_t c_at, uint32_t e_at, u32x4 &w, uint32_t &byte) {
             w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(take(c, c_step), c_at, 0, 0));

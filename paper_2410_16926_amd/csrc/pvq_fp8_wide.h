@@ -11,8 +11,8 @@ constexpr int kWideTile = 256, kWideStep = 64, kWideLds = 4 * kWideTile * kWideS
 
 enum wide_kind {
     WIDE_PRODUCT,        // A and B in blocks along the sum: A(i, r) = a[i][r], B(r, j) = b[j][r]
-    WIDE_INPUT_GRAD,     // A(i, r) = dy[i][r], B(r, j) = b[r][j]; one or two terms
-    WIDE_WEIGHT_GRAD,    // A(i, r) = dy[r][i], B(r, j) = b[r][j]
+    WIDE_INPUT_GRAD,     // A(i, r) = dy[i][r], B(r, j) = b[r][j]; a term for each piece of each dY, one after the other
+    WIDE_WEIGHT_GRAD,    // A(i, r) = dy[r][i], B(r, j) = b[r][j]; a term for each piece of an output's dY
 };
 
 // Tiles of 256 x 256, low ones of 128 x 256, or small ones of 64 x 64 (pvq_fp8_small.h), whichever take less: a step of a low tile is 64 matrix
@@ -34,11 +34,11 @@ inline wide_tiles wide_plan(int64_t rows, int64_t cols, int64_t depth, int terms
 }
 
 struct wide_args {
-    fp8_bf16 dy[2];                  // of the terms, or of the outputs; rows aligned to 16 bytes, for input gradients whole 64s or zeros behind their last value
-    fp8_blocks a, b[2];              // b: of the terms or outputs; the gate's and the up weights
+    fp8_bf16 dy[4];                  // of the pairs, each in its pieces; rows aligned to 16 bytes, for input gradients whole 64s or zeros behind their last value
+    fp8_blocks a, b[2];              // b: of the pairs; the gate's and the up weights
     fp8_matrix out[2];
     int64_t rows, cols, depth;       // of the output, and of the sum (one term's); GATED: cols are hidden units
-    int terms;                       // of the sum
+    int terms, pieces;               // of the sum, and of a pair's dY
     int tiles_i, tiles_j;
     int parts, steps_a_part;         // of a split sum, whose parts go to work
     int units;                       // tiles of all parts of all outputs
@@ -54,6 +54,18 @@ struct wide_args {
     }
     float *work;
 };
+
+// The term that a step belongs to (four at most; behind the last step whatever follows), and whose dY and whose blocks it takes.
+template <int KIND>
+__device__ inline int term_of(int step, int steps_a_term)
+{
+    if constexpr (KIND == WIDE_PRODUCT) return 0;
+    return (step >= steps_a_term) + (step >= 2 * steps_a_term) + (step >= 3 * steps_a_term);
+}
+template <int KIND>
+__device__ inline const fp8_bf16 &dy_of(const wide_args &t, int term, int out_of) { return t.dy[KIND == WIDE_INPUT_GRAD ? term : (out_of * t.pieces + term) & 3]; }
+template <int KIND>
+__device__ inline bool second_pair(const wide_args &t, int term, int out_of) { return KIND == WIDE_INPUT_GRAD ? term >= t.pieces : out_of != 0; }
 
 // Where a step's part of an operand's tile starts, and how many bytes of the matrix are left there, the upper word below zero where none are: what
 // lies behind is zero.  (Of 64 bits compared whole the vector unit does it, between matrix instructions.)
@@ -111,7 +123,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
     const int wi = wave / 2, wj = wave % 2, r16 = lane % 16, quarter = lane / 16;
     const int steps_a_term = (int)((t.depth + kWideStep - 1) / kWideStep);
 
-    // Strides in bytes (the same for both terms or outputs).  A lane's piece is eight values of a row; an operand whose rows run along the sum has eight
+    // Strides in bytes (the same for all terms and outputs).  A lane's piece is eight values of a row; an operand whose rows run along the sum has eight
     // lanes to a row, one whose rows run across it 32 (A of 128 columns 16), and piece p is 32 or 8 (16) rows behind piece p - 1.
     const uint32_t a_row = A_CODES ? (uint32_t)t.a.code_row() : (uint32_t)t.dy[0].ld * 2, b_row = (uint32_t)t.b[0].code_row();
     const uint32_t ae_row = (uint32_t)t.a.exp_row(), be_row = (uint32_t)t.b[0].exp_row();
@@ -130,11 +142,11 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
     auto stop = [&] { a_src.left_up = b_src.left_up = u_src.left_up = ae_src.left_up = be_src.left_up = ue_src.left_up = -1; };
     // where the loads are
     wide_unit ahead = unit_of(blockIdx.x);
-    int ahead_u = blockIdx.x, step = ahead.first, ahead_left = 0;      // (steps to the end of the unit or its first term)
-    auto start = [&] {                  // at the first step, and where the second term begins
+    int ahead_u = blockIdx.x, step = ahead.first, ahead_left = 0;      // (steps to the end of the unit or of a term)
+    auto start = [&] {                  // at the first step, and where another term begins
         const wide_args &t = argument<wide_args>();
-        const int term = step >= steps_a_term ? 1 : 0;
-        const bool second = (term | ahead.out_of) != 0;
+        const int term = term_of<KIND>(step, steps_a_term);
+        const bool second = second_pair<KIND>(t, term, ahead.out_of);
         const int64_t i0 = ahead.i0, j0 = ahead.j0;
         const int64_t r0 = (int64_t)(step - term * steps_a_term) * kWideStep;
         const fp8_blocks b = {second ? t.b[1].codes : t.b[0].codes, second ? t.b[1].exps : t.b[0].exps, 0, 0};
@@ -144,7 +156,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         } else {
             // (dY's last row to the end of its last 16 bytes: a load that is not whole would bring nothing)
             const int64_t row_end = ((A_ALONG ? (t.depth + kWideStep - 1) / kWideStep * kWideStep : t.rows) * 2 + 15) / 16 * 16;
-            const uint16_t *y = second ? t.dy[1].data : t.dy[0].data;
+            const uint16_t *y = dy_of<KIND>(t, term, ahead.out_of).data;
             a_src = A_ALONG ? source_of(y, a_row, t.rows, row_end, i0 * a_row + r0 * 2) : source_of(y, a_row, t.depth, row_end, r0 * a_row + i0 * 2);
         }
         if constexpr (B_ALONG) {
@@ -157,7 +169,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
             be_src = source_of(b.exps, be_row, t.depth, be_row, r0 * be_row + j0 / kFp8Block);
         }
         if (step > ahead.last) stop();
-        ahead_left = max((KIND == WIDE_INPUT_GRAD && !term ? min(steps_a_term, ahead.last + 1) : ahead.last + 1) - step, 1);
+        ahead_left = max((KIND == WIDE_PRODUCT ? ahead.last + 1 : min((term + 1) * steps_a_term, ahead.last + 1)) - step, 1);
     };
     __amdgpu_buffer_rsrc_t a_from, b_from, u_from, ae_from, be_from, ue_from;
     // (rows along the sum: an exponent is that of two steps)
@@ -172,7 +184,7 @@ __device__ __forceinline__ void wide_sums(const wide_args &t, uint8_t *lds, int 
         if (what == 2 && GATED) u_from = take(u_src, b_step);
         if (what == 3 && GATED) ue_from = take(ue_src, step & 1);
     };
-    auto go_on = [&](int steps) {                 // behind so many; on to the second term or the next unit; behind the last unit there are steps of zeros
+    auto go_on = [&](int steps) {                 // behind so many; on to the next term or unit; behind the last unit there are steps of zeros
         ahead_left -= steps;
         if (ahead_left) return;
         if (step > ahead.last) {
