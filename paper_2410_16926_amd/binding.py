@@ -506,7 +506,11 @@ def pvq_fp8_gated_backward(dH, X: Fp8Blocks, gate: Fp8Blocks, up: Fp8Blocks, G: 
     None for those not wanted.  float32 (the default) and float16 take twice the operations of bfloat16, for slopes of more bits."""
     _same_columns(X, gate)
     _same_columns(X, up)
-    _same_columns(G, U)
+    if gate.rows != up.rows:
+        raise ValueError(f"{gate.rows} and {up.rows} hidden units")
+    for b in (G, U):                        # (their planes alone would do for up to 127 columns more or less)
+        if (b.rows, b.cols) != (X.rows, gate.rows):
+            raise ValueError(f"kept products of {b.rows} x {b.cols} for {X.rows} tokens of {gate.rows} hidden units")
     if not input_grad and not weight_grads:
         return None, None, None
     return _result((_native_module or _native()).fp8_gated_backward(
