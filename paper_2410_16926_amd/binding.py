@@ -26,7 +26,7 @@ EXPORTS = [
 
 # diagnostics declared in csrc/pvq_diagnostics.h, exported for the tests
 DIAGNOSTICS = ["pvq_fast_tables_selftest", "pvq_walk_tables_selftest", "pvq_decode_gemv_plan", "pvq_correct_set_front_tiles",
-               "pvq_decode_set_table_decoder_min_groups", "pvq_decode_gemv_on", "pvq_exact_selftest"]
+               "pvq_decode_set_table_decoder_min_groups", "pvq_decode_gemv_on", "pvq_exact_selftest", "pvq_fp8_plan"]
 
 
 class PvqError(RuntimeError):
@@ -90,6 +90,7 @@ def lib():
         L.pvq_fp8_input_grad_work_bytes.argtypes = L.pvq_fp8_weight_grad_work_bytes.argtypes = [vp, i64, i64, i64, i64, vp]
         L.pvq_fp8_gated_work_bytes.argtypes = [i64, i64, i64, i32, i32, vp]
         L.pvq_fp8_gated_backward_work_bytes.argtypes = [i64, i64, i64, vp]
+        L.pvq_fp8_plan.argtypes = [i32, i64, i64, i64, i32, vp, vp]
         L.pvq_fp8_product.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
         L.pvq_fp8_input_grad.argtypes = [vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]
         L.pvq_fp8_weight_grad.argtypes = [vp, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp, sz, vp]
@@ -190,6 +191,17 @@ def pvq_decode_gemv_plan(ctx, rows: int, cols: int, batch: int):
     _check(lib().pvq_decode_gemv_plan(ctx.handle, rows, cols, batch, kinds, nvecs, 16, C.byref(n)),
            "pvq_decode_gemv_plan")
     return [(PASS_KINDS[kinds[i]], nvecs[i]) for i in range(n.value)]
+
+
+FP8_CALLS = {"product": 0, "gated": 1, "gated_to_blocks": 2, "gated_kept": 3, "input_grad": 4, "weight_grad": 5, "gated_input_grad": 6, "gated_weight_grads": 7}
+FP8_KINDS = ("rows", "tiles_64", "tiles_128", "tiles_256", "tiles_8bit")
+
+
+def pvq_fp8_plan(call: str, m: int, n: int, k: int, out_dtype: int = PVQ_BF16):
+    """(kind of tiles, parts of a sum) with which a call on 8-bit blocks takes a shape (nothing is launched; csrc/pvq_diagnostics.h)."""
+    kind, parts = C.c_int(), C.c_int()
+    _check(lib().pvq_fp8_plan(FP8_CALLS[call], m, n, k, out_dtype, C.byref(kind), C.byref(parts)), "pvq_fp8_plan")
+    return FP8_KINDS[kind.value], parts.value
 
 
 def pvq_size_table_device(D: int, K: int, words: int, device=None):

@@ -82,6 +82,20 @@ enum { PVQ_EXACT_RECIPROCAL = 0, PVQ_EXACT_ROOT = 1, PVQ_EXACT_SMALL_OVER = 2, P
        PVQ_EXACT_DIVIDE = 5 };
 int pvq_exact_selftest(int what, uint32_t k, uint64_t first, uint64_t count, uint64_t *mismatches, void *stream);
 
+/*
+ * How the calls on 8-bit blocks divide a shape, without launching anything (the tests of a kind of tile make sure by it that they reach one).
+ * what: the call; m, n, k as in it; out_dtype its result's type.  *kind (host) receives what takes it, *parts (host) into how many parts its
+ * sums are split.  Of the gated block's backward pass the two halves are asked for one by one.  PVQ_E_INVALID_ARG for NULL, sizes below 1 and what is
+ * not in the lists, PVQ_E_UNSUPPORTED as the calls have it.
+ */
+enum { PVQ_FP8_PRODUCT = 0, PVQ_FP8_GATED = 1, PVQ_FP8_GATED_TO_BLOCKS = 2, PVQ_FP8_GATED_KEPT = 3, PVQ_FP8_INPUT_GRAD = 4, PVQ_FP8_WEIGHT_GRAD = 5,
+       PVQ_FP8_GATED_INPUT_GRAD = 6, PVQ_FP8_GATED_WEIGHT_GRADS = 7 };
+enum { PVQ_FP8_BY_ROWS = 0,           /* few rows: weights streamed, the bfloat16 instruction */
+       PVQ_FP8_TILES_64 = 1,          /* tiles of 64 x 64, of 128 x 256 and of 256 x 256 on the bfloat16 instruction */
+       PVQ_FP8_TILES_128 = 2, PVQ_FP8_TILES_256 = 3,
+       PVQ_FP8_TILES_8BIT = 4 };      /* tiles of 256 x 256 on the 8-bit instruction */
+int pvq_fp8_plan(int what, int64_t m, int64_t n, int64_t k, int out_dtype, int *kind, int *parts);
+
 #ifdef __cplusplus
 }
 #endif

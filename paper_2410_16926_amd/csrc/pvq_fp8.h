@@ -81,6 +81,9 @@ struct fp8_product_args {
     float *work;
 };
 size_t fp8_product_work(int64_t m, int64_t n, int64_t k, int out_dtype);
+// the tiles that a product or the gated block takes (rows of 0: 256 on the 8-bit instruction) and the parts of their sums
+struct fp8_tiles { int rows, parts; };
+fp8_tiles fp8_product_tiles(int64_t m, int64_t n, int64_t k, bool gated, bool wide, bool to_blocks);
 hipError_t fp8_launch_product(const fp8_product_args &a, hipStream_t s);
 
 // H = act(X Wg^T) * (X Wu^T); h in floats (h.data) or in blocks (hc, he), and G and U in blocks where gc, ge, uc and ue are given
@@ -91,7 +94,11 @@ struct fp8_gated_args {
     uint8_t *hc, *he, *gc, *ge, *uc, *ue;
     float *work;
 };
-// wide: sums on the bfloat16 instruction (float32 results, kept products); to_blocks: H in blocks, or G and U kept
+// Whether the gated block's sums are formed on the bfloat16 instruction whatever their number: for float32 results, and with kept products.  These
+// are codes of sums of 32 bits: what the 8-bit instructions are off would change one code of 2000, which is as much again as the roundings of
+// the gradients to bfloat16 (dX 3.0e-3 off instead of 2.3e-3).
+inline bool fp8_gated_is_wide(bool kept, bool in_floats, int out_dtype) { return kept || (in_floats && out_dtype == PVQ_F32); }
+// wide: as above; to_blocks: H in blocks, or G and U kept
 size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide, bool to_blocks);
 hipError_t fp8_launch_gated(const fp8_gated_args &a, hipStream_t s);
 // ... of the parts of G and U, [parts][2][rows][cols]
@@ -120,6 +127,8 @@ struct fp8_grad_args {
 // whether a single gradient's dY is taken with rows that start and end anywhere
 bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k);
 bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k);
+fp8_tiles fp8_input_grad_tiles(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
+fp8_tiles fp8_weight_grad_tiles(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
 size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
 size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces);
 hipError_t fp8_launch_input_grad(const fp8_grad_args &a, hipStream_t s);

@@ -63,6 +63,9 @@ hipError_t launch(wide_args &t, const fp8_grad_args &g, int outputs, hipStream_t
 static bool as_it_is(const wide_tiles &plan) { return plan.rows == kSmallTile && plan.us < 14.0; }
 bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k) { return as_it_is(wide_plan(m, k, n, 1, 1)); }
 bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k) { return as_it_is(wide_plan(n, k, m, 1, 1)); }
+static fp8_tiles tiles_of(const wide_tiles &t) { return {t.rows, t.parts}; }
+fp8_tiles fp8_input_grad_tiles(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return tiles_of(wide_plan(m, k, n, pairs * pieces, 1)); }
+fp8_tiles fp8_weight_grad_tiles(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return tiles_of(wide_plan(n, k, m, pieces, pairs)); }
 size_t fp8_input_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return work_of(m, k, n, pairs * pieces, 1); }
 size_t fp8_weight_grad_work(int64_t m, int64_t n, int64_t k, int pairs, int pieces) { return work_of(n, k, m, pieces, pairs); }
 

@@ -1,4 +1,5 @@
 // 8-bit blocks: the C entries, checks of their arguments.
+#include "pvq_diagnostics.h"
 #include "pvq_fp8.h"
 
 namespace {
@@ -61,6 +62,9 @@ constexpr int kMostPieces = 2;
 // Whether the gradient kernels of large tiles can take dY as it is: rows aligned to 16 bytes, a tile's within 32-bit offsets, and where they run along
 // the sum (dX) in whole steps of it.  Otherwise it is copied first, with zeros behind the rows.
 bool whole_rows(const void *dY, int64_t ld, int64_t n, bool along) { return aligned(dY, 16) && ld % 8 == 0 && ld <= kMostCols && (!along || n % 64 == 0); }
+
+// whether the kernel that streams the weights takes the gated block
+bool gated_by_rows(int64_t m, bool to_blocks, int64_t k) { return fp8_rows_pay(m) && !to_blocks && k > 0; }
 
 size_t up16(size_t v) { return (v + 15) / 16 * 16; }
 
@@ -226,7 +230,7 @@ extern "C" int pvq_fp8_gated(const uint8_t *x_codes, const uint8_t *x_exponents,
                                  encoded ? check_blocks({h_codes, h_exponents, m, n}) : PVQ_OK, keep ? check_blocks({g_codes, g_exponents, m, n}) : PVQ_OK,
                                  keep ? check_blocks({u_codes, u_exponents, m, n}) : PVQ_OK, check_work(work, work_bytes, wanted)}))
         return rc;
-    return status_of(fp8_rows_pay(m) && !keep && !encoded && k > 0 ? fp8_launch_gated_rows(a, (hipStream_t)stream) : fp8_launch_gated(a, (hipStream_t)stream));
+    return status_of(gated_by_rows(m, keep || encoded, k) ? fp8_launch_gated_rows(a, (hipStream_t)stream) : fp8_launch_gated(a, (hipStream_t)stream));
 }
 
 extern "C" int pvq_fp8_gated_backward_work_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes)
@@ -290,4 +294,32 @@ extern "C" int pvq_fp8_gated_backward(const void *dH, int64_t lddh, const uint8_
         e = fp8_launch_weight_grad(a, s);
     }
     return status_of(e);
+}
+
+extern "C" int pvq_fp8_plan(int what, int64_t m, int64_t n, int64_t k, int out_dtype, int *kind, int *parts)
+{
+    if (m < 1 || n < 1 || k < 1 || !known(out_dtype) || !kind || !parts) return PVQ_E_INVALID_ARG;
+    if (const int rc = first_of({check_shape(m, k), check_shape(n, k), what == PVQ_FP8_PRODUCT ? check_result(m, n) : check_shape(m, n)})) return rc;
+    const int pieces = slope_pieces(out_dtype);
+    const bool to_blocks = what == PVQ_FP8_GATED_TO_BLOCKS || what == PVQ_FP8_GATED_KEPT;
+    fp8_tiles t{};
+    bool by_rows = false;
+    switch (what) {
+    case PVQ_FP8_PRODUCT:
+        by_rows = fp8_rows_pay(m);
+        t = fp8_product_tiles(m, n, k, false, out_dtype == PVQ_F32, false);
+        break;
+    case PVQ_FP8_GATED: case PVQ_FP8_GATED_TO_BLOCKS: case PVQ_FP8_GATED_KEPT:
+        by_rows = gated_by_rows(m, to_blocks, k);
+        t = fp8_product_tiles(m, n, k, true, fp8_gated_is_wide(what == PVQ_FP8_GATED_KEPT, what != PVQ_FP8_GATED_TO_BLOCKS, out_dtype), to_blocks);
+        break;
+    case PVQ_FP8_INPUT_GRAD: t = fp8_input_grad_tiles(m, n, k, 1, 1); break;
+    case PVQ_FP8_WEIGHT_GRAD: t = fp8_weight_grad_tiles(m, n, k, 1, 1); break;
+    case PVQ_FP8_GATED_INPUT_GRAD: t = fp8_input_grad_tiles(m, n, k, 2, pieces); break;
+    case PVQ_FP8_GATED_WEIGHT_GRADS: t = fp8_weight_grad_tiles(m, n, k, 2, pieces); break;
+    default: return PVQ_E_INVALID_ARG;
+    }
+    *kind = by_rows ? PVQ_FP8_BY_ROWS : t.rows == 0 ? PVQ_FP8_TILES_8BIT : t.rows == 64 ? PVQ_FP8_TILES_64 : t.rows == 128 ? PVQ_FP8_TILES_128 : PVQ_FP8_TILES_256;
+    *parts = by_rows ? 1 : t.parts;
+    return PVQ_OK;
 }

@@ -372,6 +372,11 @@ hipError_t launch_tiles(const fp8_blocks &a, const fp8_blocks &b, const fp8_bloc
 
 }  // namespace
 
+fp8_tiles fp8_product_tiles(int64_t m, int64_t n, int64_t k, bool gated, bool wide, bool to_blocks)
+{
+    const wide_tiles t = plan_of(m, n, k, gated, wide, to_blocks).tiles;
+    return {t.rows, t.parts};
+}
 size_t fp8_product_work(int64_t m, int64_t n, int64_t k, int out_dtype) { return fp8_rows_pay(m) ? 0 : work_of(m, n, k, false, out_dtype == PVQ_F32, false); }
 size_t fp8_gated_work(int64_t m, int64_t n, int64_t k, bool wide, bool to_blocks) { return work_of(m, n, k, true, wide, to_blocks); }
 
@@ -389,10 +394,7 @@ hipError_t fp8_launch_gated(const fp8_gated_args &g, hipStream_t s)
     tile_out out{};
     out.gated = {g.h, g.act, g.hc, g.he, g.gc, g.ge, g.uc, g.ue};
     out.work = g.work;
-    // Kept products are codes of sums of 32 bits: what the 8-bit instructions are off would change one code of 2000, which is as
-    // much again as the roundings of the gradients to bfloat16 (dX 3.0e-3 off instead of 2.3e-3).
-    const bool wide = g.gc || (g.h.data && g.h.dtype == PVQ_F32);
-    hipError_t e = launch_tiles<true>(g.x, g.gate, g.up, out, wide, g.gc || g.hc, s);
+    hipError_t e = launch_tiles<true>(g.x, g.gate, g.up, out, fp8_gated_is_wide(g.gc != nullptr, g.h.data != nullptr, g.h.dtype), g.gc || g.hc, s);
     if (out.parts && e == hipSuccess) e = fp8_launch_gated_join(g.work, out.parts, g, s);
     return e;
 }
