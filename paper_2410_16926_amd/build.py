@@ -2,7 +2,9 @@
 torch.  The library needs neither torch nor Python's headers."""
 from __future__ import annotations
 
+import glob
 import os
+import re
 import subprocess
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
@@ -21,6 +23,11 @@ SOURCES = ["pvq_host.cpp", "pvq_fast8_tables.cpp", "pvq_kernels.hip", "pvq_fast8
 
 HEADERS = ["pvq_internal.h", "pvq_fast8.h", "pvq_hadamard_dev.h", "pvq_quantize_dev.h", "pvq_diagnostics.h", "pvq_small_table.h",
            "pvq_walk.h", "pvq_exact_dev.h", "pvq_fp8.h", "pvq_fp8_dev.h", "pvq_fp8_tile.h", "pvq_fp8_wide.h", "pvq_fp8_small.h"]
+
+# Kernels whose sums lie in accumulation registers that assembly statements write (csrc/pvq_fp8_tile.h).  The compiler knows of no wait between these
+# and what reads the registers, so a library is linked only of code in which it has left them alone.
+SUMS_IN_ASSEMBLY = ["pvq_fp8_product.hip", "pvq_fp8_grad.hip"]
+KEEP_LISTING = "--save-temps=obj"
 
 # -ffp-contract=off: the encoder's float32 results are part of the format (no fused multiply-adds
 # unless written as fmaf); correctly rounded float32 division and square root likewise.
@@ -69,7 +76,77 @@ def _run(cmd):
     err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
     if res.returncode != 0:
         raise RuntimeError("compilation failed:\n" + " ".join(cmd) + "\n" + err)
+    if KEEP_LISTING in cmd:
+        _check_listing(cmd[cmd.index("-o") + 1])
     return err
+
+
+def _registers(operands: str) -> set:
+    """The vector registers in a text of operands."""
+    out = set()
+    for first, last, one in re.findall(r"\bv\[(\d+):(\d+)\]|\bv(\d+)\b", operands):
+        out |= set(range(int(first), int(last) + 1)) if first else {int(one)}
+    return out
+
+
+def disturbed_sums(listing: str) -> list:
+    """What in the assembly listing of a source of SUMS_IN_ASSEMBLY could make its sums wrong: registers kept in memory, accumulation registers
+    moved, read anywhere but in the statements that wait for them, or written with anything but zeros in front of the matrix
+    instructions; and a matrix instruction of a statement within two wait states of a vector instruction that writes an operand
+    of it, which for its own ones the compiler keeps apart."""
+    wrong, kernels = [], list(re.finditer(r"^(_ZN\S*?\d(?:wide_tile_kernel|tile_kernel|grad_kernel)\S*):", listing, re.M))
+    if not kernels:
+        wrong.append("no kernels found")
+    for m in kernels:
+        lines = [line.strip() for line in listing[m.end():listing.index(".end_amdhsa_kernel", m.end())].split("\n")]
+        code = [line if line == ";;#ASMSTART" else line.split(";")[0].strip() for line in lines]
+        code = [line for line in code if line and (not line.startswith(".") or line.endswith(":"))]
+        matrix = [i for i, line in enumerate(code) if line.startswith("v_mfma")]
+        labels = {line[:-1]: i for i, line in enumerate(code) if line.endswith(":")}
+        from_behind = {}
+        for i, line in enumerate(code):
+            if line.startswith(("s_branch", "s_cbranch")) and line.split()[1] in labels:
+                from_behind.setdefault(labels[line.split()[1]], []).append(i)
+
+        def writers(at, states, operands):
+            """Vector instructions that write one of the operands within so many wait states in front of `at`, by way of jumps too."""
+            found = []
+            before = [at - 1] if at and not code[at - 1].startswith(("s_branch", "s_endpgm")) else []
+            for i in before + from_behind.get(at, []):
+                line = code[i]
+                name, _, rest = line.partition(" ")
+                if name.startswith("v_") and not name.startswith(("v_mfma", "v_accvgpr")) and _registers(rest.split(",")[0]) & operands:
+                    found.append(line)
+                    continue
+                left = states - (0 if line.endswith(":") or line == ";;#ASMSTART" else int(rest, 0) + 1 if name == "s_nop" else 1)
+                if left > 0:
+                    found += writers(i, left, operands)
+            return found
+
+        for i, line in enumerate(code):
+            bad = line.startswith(("scratch_", "v_accvgpr_mov")) or (line.startswith("v_accvgpr_read") and code[i - 1] != ";;#ASMSTART")
+            bad = bad or (line.startswith("v_accvgpr_write") and matrix and i < matrix[-1] and not line.endswith(", 0"))
+            bad = bad or (i in matrix and writers(i, 2, _registers(line.partition(",")[2])))
+            if bad:
+                wrong.append(f"{m.group(1)}: {line}")
+    return wrong
+
+
+def _check_listing(obj: str):
+    """Looks at the listing that was kept beside an object, and leaves nothing but the object."""
+    name = os.path.basename(obj)
+    kept = [path for stem in (name[:name.index(".")], name[:-2]) for path in glob.glob(os.path.join(os.path.dirname(obj), stem + "-h*"))]
+    text = ""
+    for path in kept:
+        if path.endswith("gfx950.s"):
+            with open(path) as f:
+                text += f.read()
+    for path in kept:
+        os.remove(path)
+    wrong = disturbed_sums(text)
+    if wrong:
+        os.remove(obj)
+        raise RuntimeError(f"this compiler's code for {name} could form wrong sums:\n" + "\n".join(wrong[:20]))
 
 
 def _have_torch() -> bool:
@@ -113,7 +190,8 @@ def build(force: bool = True, verbose: bool = False, library: bool = True, bindi
     if library:
         for src in sources():
             objs.append(os.path.join(objdir, os.path.basename(src) + ".o"))
-            jobs.append([hipcc, *compile_flags, "-x", "hip", f"-I{_INC}", f"-I{_CSRC}", "-c", src, "-o", objs[-1]])
+            keep = [KEEP_LISTING] if os.path.basename(src) in SUMS_IN_ASSEMBLY else []
+            jobs.append([hipcc, *compile_flags, *keep, "-x", "hip", f"-I{_INC}", f"-I{_CSRC}", "-c", src, "-o", objs[-1]])
     if binding:
         torch_obj = os.path.join(objdir, "pvq_torch.cpp.o")
         jobs.append(_torch_object_command(torch_obj))
