@@ -319,8 +319,8 @@ int pvq_decode_gemv(const pvq_ctx *ctx, const uint32_t *index, const void *scale
  * instruction multiplies them in by itself, and because every decoded value is then exact in bfloat16.
  *
  * Everywhere below: codes 16-byte aligned, exponents 4-byte aligned; matrices of floats aligned to their element, any ld >= cols
- * (rows that are aligned to 16 bytes are faster, and are read to the end of their last 16 bytes); rows or cols may be 0; columns of a block matrix at most 4194304 (2^22),
- * rows at most 2^30 and values 2^41, else PVQ_E_UNSUPPORTED.
+ * (rows that are aligned to 16 bytes are faster, and are read to the end of their last 16 bytes); rows or cols may be 0; columns of a block matrix, of dY and
+ * of dH at most 4194304 (2^22), rows at most 2^30 and values 2^41, else PVQ_E_UNSUPPORTED.
  * Calls are asynchronous, launch kernels on `stream` only and may be captured.  NaN codes give NaN; codes behind the last
  * column that are not zero and exponent bytes outside 17 .. 247 (which encoding never writes) give unspecified values, never
  * an out-of-bounds access.
@@ -347,8 +347,10 @@ int pvq_fp8_decode(const uint8_t *codes, const uint8_t *exponents, int64_t rows,
  * Y = A B^T, A [m][k] and B [n][k] in blocks, Y [m][ldy] of out_dtype: tokens times weights, any number of tokens.
  * Sums are float32.  To PVQ_F32 they are formed of the decoded values by the bfloat16 matrix instructions; to PVQ_BF16 and PVQ_F16
  * by the 8-bit ones, which align the products of a group of eight to the largest among them and drop what lies 14 bits below
- * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4); few rows of A (up to 32) and small
- * products take the bfloat16 instructions for every type.  The order of the sums depends on the shape alone.
+ * (3e-5 of a sum of Gaussian terms, the output's own rounding being 1.7e-3 and 2e-4; 1e-4 where a few columns are a thousand times as large as the others.
+ * It goes by the size of the terms: a sum of terms that cancel is off by as much, so that its relative error may exceed the output's rounding;
+ * PVQ_F32 has none of this); few rows of A (up to 32) and small products take the bfloat16 instructions for every type: a row's results of other
+ * numbers of rows differ by that much.  The order of the sums depends on the shape alone.
  *   work   device, 16-byte aligned scratch of pvq_fp8_product_work_bytes bytes (may be NULL where that is 0); calls that
  *          may overlap in time need one each
  * k == 0 gives zeros.
@@ -374,15 +376,19 @@ int pvq_fp8_weight_grad(const void *dY, int64_t lddy, int64_t m, int64_t n, cons
                         int64_t k, void *dW, int out_dtype, int64_t lddw, void *work, size_t work_bytes, void *stream);
 
 /*
- * The first half of a gated feed-forward block in one kernel: H = act(G) * U, G = X Wg^T, U = X Wu^T, with X [m][k],
- * Wg and Wu [n][k] in blocks; G and U stay in registers, in float32.
+ * The first half of a gated feed-forward block in one call: H = act(G) * U, G = X Wg^T, U = X Wu^T, with X [m][k],
+ * Wg and Wu [n][k] in blocks.  Large shapes, and with H in floats alone few rows (up to 32) and small shapes, take one kernel, in which G and U
+ * stay in registers, in float32.  Where the sums are split, and for small shapes with results in blocks, their float32 sums pass through work,
+ * 8 m n bytes for each part, and a second kernel adds them and makes of them what is wanted.  (Few rows: H to floats and pvq_fp8_encode behind it take
+ * less than H in blocks, 95 us instead of 114 for one row of 28672 x 8192.)
  *   PVQ_SILU  act(g) = g / (1 + exp(-g))
  *   PVQ_GELU  act(g) = 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
  *   H                    device, [m][ldh] of out_dtype, or NULL
  *   h_codes, h_exponents H in blocks (the input of the product behind it), or NULL both; one of H and these is wanted
  *   g_codes .. u_exponents   G and U in blocks, what the backward pass needs of them, or NULL all four
  * Sums as in pvq_fp8_product, by the type of H (the 8-bit instructions where there is none), with G and U kept those of PVQ_F32.
- *   work                 as for pvq_fp8_product; to_blocks: not zero where H is wanted in blocks or G and U are kept
+ *   work                 as for pvq_fp8_product; to_blocks: not zero where H is wanted in blocks or G and U are kept.  The size is enough for
+ *                        either instruction, whichever the call takes
  */
 typedef enum { PVQ_SILU = 0, PVQ_GELU = 1 } pvq_activation;
 int pvq_fp8_gated_work_bytes(int64_t m, int64_t n, int64_t k, int out_dtype, int to_blocks, size_t *bytes);

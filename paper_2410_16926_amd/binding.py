@@ -494,8 +494,8 @@ def pvq_fp8_weight_grad(dY, X: Fp8Blocks, out_dtype=None, out=None):
 
 def pvq_fp8_gated(X: Fp8Blocks, gate: Fp8Blocks, up: Fp8Blocks, activation: str = "silu", out_dtype=None, out=None, keep: bool = False,
                   encode: bool = False):
-    """H = activation(X gate^T) * (X up^T) in one kernel; activation "silu" or "gelu" (its tanh form).  H is a tensor of out_dtype, or
-    with encode=True in 8-bit blocks, as the product behind it takes it.  keep=True: (H, G, U) with the two products in 8-bit
+    """H = activation(X gate^T) * (X up^T), for large shapes in one kernel; activation "silu" or "gelu" (its tanh form).  H is a tensor of out_dtype, or
+    with encode=True in 8-bit blocks, as the product behind it takes it (up to 32 rows are faster to bfloat16, with pvq_fp8_encode behind).  keep=True: (H, G, U) with the two products in 8-bit
     blocks, which pvq_fp8_gated_backward takes."""
     _same_columns(X, gate)
     _same_columns(X, up)
