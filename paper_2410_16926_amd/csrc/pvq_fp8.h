@@ -104,12 +104,14 @@ hipError_t fp8_launch_gated(const fp8_gated_args &a, hipStream_t s);
 // ... of the parts of G and U, [parts][2][rows][cols]
 hipError_t fp8_launch_gated_join(const float *work, int parts, const fp8_gated_args &a, hipStream_t s);
 
-// Few rows of A (tokens): the kernels that stream B (pvq_fp8_rows.hip).  Called by the two above.
+// Few rows of A (tokens): the kernels that stream B (pvq_fp8_rows.hip).  The entries of pvq_fp8_host.cpp choose between these and the two above.
 bool fp8_rows_pay(int64_t m);
 hipError_t fp8_launch_product_rows(const fp8_product_args &a, hipStream_t s);
 hipError_t fp8_launch_gated_rows(const fp8_gated_args &a, hipStream_t s);
 
-// A bf16 matrix [rows][cols] with row stride ld.  (The gradient kernels take rows aligned to 16 bytes, of at most 2^22 values.)
+// A bf16 matrix [rows][cols] with row stride ld.  The gradients' large tiles take rows aligned to 16 bytes and strides of at most 2^22 values, dX whole 64s
+// of the sum or zeros behind a row; their small tiles rows that start and end anywhere, of any stride.  pvq_fp8_host.cpp sees to it (copy_bytes,
+// take_dy): what is not so is copied, but for small tiles that are faster without (fp8_input_grad_as_it_is, fp8_weight_grad_as_it_is).
 struct fp8_bf16 {
     const uint16_t *data = nullptr;
     int64_t rows = 0, cols = 0, ld = 0;
@@ -124,7 +126,7 @@ struct fp8_grad_args {
     fp8_matrix out[2];
     float *work;
 };
-// whether a single gradient's dY is taken with rows that start and end anywhere
+// whether a single gradient's dY is taken with rows that start and end anywhere, by small tiles
 bool fp8_input_grad_as_it_is(int64_t m, int64_t n, int64_t k);
 bool fp8_weight_grad_as_it_is(int64_t m, int64_t n, int64_t k);
 fp8_tiles fp8_input_grad_tiles(int64_t m, int64_t n, int64_t k, int pairs, int pieces);

@@ -10,7 +10,7 @@ constexpr int kSmallTile = 64, kSmallPlane = kSmallTile * kWideStep * 2, kSmallL
 // Four waves of 32 x 32.  A step is 64 of the sum, and little but waiting and the instructions of one wave a SIMD: a thread's sixteen values of either operand
 // are fetched four steps ahead (six or eight: longer to start, 2 to 8 % more), decoded and put into one of two stages; one barrier a step, 0.3 us alone on a unit, 0.21 of several
 // that take turns (where a step starts worked out anew each time, 0.35 to 0.45).  64 x 1500 x 1500 10.5 us, in large tiles 23; the gated block of 64 x 1500 x 1500 with G and U
-// kept 14 and 43; but it reads four times what large tiles do: 333 x 3001 x 11008 69 us, in tiles of 128 x 256 46.
+// kept 13 and 43; but it reads four times what large tiles do: 333 x 3001 x 11008 69 us, in tiles of 128 x 256 46.
 // dY's rows may start anywhere: they are loaded as they lie, what is behind their end by elements.
 template <int KIND, bool GATED>
 __device__ __forceinline__ void small_sums(const wide_args &t, uint8_t *lds, const wide_unit &u, f32x4 (&acc)[2][2])

@@ -34,7 +34,7 @@ inline wide_tiles wide_plan(int64_t rows, int64_t cols, int64_t depth, int terms
 }
 
 struct wide_args {
-    fp8_bf16 dy[4];                  // of the pairs, each in its pieces; rows aligned to 16 bytes, for input gradients whole 64s or zeros behind their last value
+    fp8_bf16 dy[4];                  // of the pairs, each in its pieces, all of one stride; how their rows lie: fp8_bf16
     fp8_blocks a, b[2];              // b: of the pairs; the gate's and the up weights
     fp8_matrix out[2];
     int64_t rows, cols, depth;       // of the output, and of the sum (one term's); GATED: cols are hidden units
